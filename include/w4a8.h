@@ -383,6 +383,67 @@ int w4a8_linear_silu_mul_fp8_out(const uint8_t* x8_dev, int64_t M, int64_t K, in
                                  const uint8_t* packed_dev, const float* w_scales_dev, int64_t F, int32_t group_size,
                                  const float* h_scale_dev, uint8_t* h8_dev, int64_t ldh8, void* stream);
 
+/*
+ * Attention between a block's QKV and O layers, and its key/value cache.  All tensors bf16 unless stated.  H query heads share HK key and
+ * value heads, H / HK of them each (query head h reads key head h / (H / HK)); D channels per head, 64 or 128; H <= 4096.
+ *   cache       keys and values each in pages of P tokens, a page [HK, P, D] row-major, page p at p * page_stride elements
+ *               (page_stride >= HK * P * D, whole 16-byte pieces; 16-byte aligned); P a power of two, 16 .. 1024; n_pages * P <= 2^30.
+ *               Elements bf16, or E4M3 bytes that stand for byte * kv_scales_dev[0] (keys), byte * kv_scales_dev[1] (values): static
+ *               per-tensor scales, as for activations (Eq. 13).  kv_scales_dev is read for E4M3 only
+ *   tables_dev  int32 page numbers: position j of a sequence is token j % P of page table[j / P].  Sequences may list the same page
+ *   rows        row strides (ld*) in elements, below 2^20; rows are 16-byte aligned (pointer and stride)
+ *
+ * w4a8_rope_cache_write: for each token t of a QKV layer's output, qkv_dev [T, (H + 2 HK) * D] (query heads, key heads, value heads),
+ *   turns every query and key head by the angles of row positions_dev[t] of cos_sin_dev (float32 [table_rows, D]: D/2 cosines, then
+ *   D/2 sines; 16-byte aligned),
+ *     (a, b) -> (a cos - b sin, b cos + a sin),  channels (i, i + D/2) (W4A8_ROPE_HALVES) or (2i, 2i + 1) (W4A8_ROPE_PAIRS),
+ *   in float32, rounded once: queries to q_out_dev [T, H * D], keys to k_out_dev [T, HK * D] (NULL: not kept as rows) and, with the
+ *   values, to slot slots_dev[t] of the cache, page slot / P, token slot % P: rounded to bf16, or nearest_E4M3(x / scale), one float32 division
+ *   of the rotated float32 value.  A token whose slot is outside [0, n_pages * P) is padding: nothing is read or written for it.  A position
+ *   outside the table gives NaN.  The slots of a call are distinct.  q_out_dev may be qkv_dev itself (ldq = ldqkv), and k_out_dev its key columns.
+ *   T <= 2^24.
+ *
+ * w4a8_attention_prompt: n_seqs whole prompts packed in rows, sequence s being rows starts_dev[s] .. starts_dev[s + 1] - 1 (int32,
+ *   n_seqs + 1 of them, not decreasing, within [0, T]; lengths of zero are allowed):
+ *     y[i] = sum_j softmax_j(softmax_scale * q[i] . k[j]) v[j]  over the rows j of i's sequence, j <= i if causal = 1.
+ *   Rows of no sequence (before the first, behind the last) are left as they were.  What a row may not see has no effect on it,
+ *   infinities and NaN included.  q_dev [T, H * D], k_dev and v_dev [T, HK * D].  Scores, their maximum and sum and the output's sum are
+ *   float32; the weights enter the second product as bf16.  y_scale_dev NULL: y_dev is bf16 [T, H * D].  Otherwise E4M3 bytes, those of
+ *   w4a8_quantize_act of that output with *y_scale_dev.  0 < softmax_scale <= 1e30.  T <= 2^24.
+ *
+ * w4a8_attention_decode: one token of each of n_seqs sequences, q_dev [n_seqs, H * D], against the prefix_length tokens that the pages
+ *   prefix_pages_dev hold, common to all (computed once for the batch; prefix_length 0: none), followed by the first lengths_dev[b]
+ *   tokens (int32) of the pages of its own table, row b of tables_dev [n_seqs, table_width], row stride ld_tables.  Lengths count up to
+ *   table_width * P.  A page number outside [0, n_pages) holds no tokens.  A sequence without any token gives zeros.  The tokens behind a length may
+ *   hold anything.  Precision and y as above.  Lengths, tables and page numbers are read on the device: a captured launch follows them.
+ *   workspace_dev: w4a8_attention_decode_workspace_bytes() bytes for these sizes (W4A8_ERR_WORKSPACE if fewer), 16-byte aligned, NULL if that
+ *   is 0; scratch, owned by the call until the stream work completes; calls that may overlap need one each.  n_seqs * H <= 2^18.
+ *
+ * w4a8_cache_copy_pages: page src_pages_dev[i] -> dst_pages_dev[i], page_bytes bytes (a multiple of 16), in each of n_planes planes (keys
+ *   and values of every layer, say): page p of plane l at l * plane_stride + p * page_stride bytes.  The destinations of a call are
+ *   distinct and none of them is also a source.  A pair with a page outside [0, n_pages) is skipped.  n_copies <= n_pages.
+ */
+typedef enum { W4A8_CACHE_BF16 = 0, W4A8_CACHE_E4M3 = 1, W4A8_CACHE_RANGE_LO = -0x7FFFFFFF - 1, W4A8_CACHE_RANGE_HI = 0x7FFFFFFF } w4a8_cache_dtype;
+typedef enum { W4A8_ROPE_HALVES = 0, W4A8_ROPE_PAIRS = 1, W4A8_ROPE_RANGE_LO = -0x7FFFFFFF - 1, W4A8_ROPE_RANGE_HI = 0x7FFFFFFF } w4a8_rope;
+int w4a8_rope_cache_write(const void* qkv_dev, int64_t T, int64_t ldqkv, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                          const float* cos_sin_dev, int64_t table_rows, w4a8_rope rope, const int32_t* positions_dev,
+                          const int32_t* slots_dev, void* q_out_dev, int64_t ldq, void* k_out_dev, int64_t ldk, void* k_cache_dev,
+                          void* v_cache_dev, w4a8_cache_dtype cache_dtype, const float* kv_scales_dev, int64_t n_pages,
+                          int64_t page_stride, int32_t page_size, void* stream);
+int w4a8_attention_prompt(const void* q_dev, int64_t ldq, const void* k_dev, int64_t ldk, const void* v_dev, int64_t ldv,
+                          const int32_t* starts_dev, int64_t n_seqs, int64_t T, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                          int32_t causal, float softmax_scale, void* y_dev, int64_t ldy, const float* y_scale_dev, void* stream);
+size_t w4a8_attention_decode_workspace_bytes(int64_t n_seqs, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t page_size,
+                                             int64_t table_width, int64_t prefix_length);
+int w4a8_attention_decode(const void* q_dev, int64_t ldq, int64_t n_seqs, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                          const void* k_cache_dev, const void* v_cache_dev, w4a8_cache_dtype cache_dtype, const float* kv_scales_dev,
+                          int64_t n_pages, int64_t page_stride, int32_t page_size, const int32_t* tables_dev, int64_t table_width,
+                          int64_t ld_tables, const int32_t* lengths_dev, const int32_t* prefix_pages_dev, int64_t prefix_length,
+                          float softmax_scale, void* y_dev, int64_t ldy, const float* y_scale_dev, void* workspace_dev,
+                          size_t workspace_bytes, void* stream);
+int w4a8_cache_copy_pages(void* cache_dev, int64_t n_planes, int64_t plane_stride, int64_t n_pages, int64_t page_stride, int64_t page_bytes,
+                          const int32_t* src_pages_dev, const int32_t* dst_pages_dev, int64_t n_copies, void* stream);
+
 /* Static, NUL-terminated description of a status value. */
 const char* w4a8_status_string(int status);
 

@@ -18,6 +18,8 @@ LIB_PATH = os.path.join(HERE, "libw4a8.so")
 F32, BF16 = 0, 1
 SRC_F32_RTN, SRC_I8_CODES, SRC_F32_RTN_POW2 = 0, 1, 2
 LAYOUT_CANONICAL, LAYOUT_TILED = 0, 1
+CACHE_BF16, CACHE_E4M3 = 0, 1
+ROPE_HALVES, ROPE_PAIRS = 0, 1
 
 _c_i64, _c_i32, _c_vp, _c_sz = ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t
 
@@ -77,6 +79,15 @@ SIGNATURES = {
     "w4a8_linear_silu_mul_fp8_out": (_c_i32, [_c_vp, _c_i64, _c_i64, _c_i64, _c_vp, _c_vp, _c_vp, _c_i64, _c_i32, _c_vp,
                                               _c_vp, _c_i64, _c_vp]),
     "w4a8_silu_mul_quantize": (_c_i32, [_c_vp, _c_i64, _c_i64, _c_i64, _c_vp, _c_vp, _c_i64, _c_vp]),
+    "w4a8_rope_cache_write": (_c_i32, [_c_vp, _c_i64, _c_i64, _c_i32, _c_i32, _c_i32, _c_vp, _c_i64, _c_i32, _c_vp, _c_vp, _c_vp, _c_i64,
+                                       _c_vp, _c_i64, _c_vp, _c_vp, _c_i32, _c_vp, _c_i64, _c_i64, _c_i32, _c_vp]),
+    "w4a8_attention_prompt": (_c_i32, [_c_vp, _c_i64, _c_vp, _c_i64, _c_vp, _c_i64, _c_vp, _c_i64, _c_i64, _c_i32, _c_i32, _c_i32, _c_i32,
+                                       ctypes.c_float, _c_vp, _c_i64, _c_vp, _c_vp]),
+    "w4a8_attention_decode_workspace_bytes": (_c_sz, [_c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_i64, _c_i64]),
+    "w4a8_attention_decode": (_c_i32, [_c_vp, _c_i64, _c_i64, _c_i32, _c_i32, _c_i32, _c_vp, _c_vp, _c_i32, _c_vp, _c_i64, _c_i64, _c_i32,
+                                       _c_vp, _c_i64, _c_i64, _c_vp, _c_vp, _c_i64, ctypes.c_float, _c_vp, _c_i64, _c_vp, _c_vp, _c_sz,
+                                       _c_vp]),
+    "w4a8_cache_copy_pages": (_c_i32, [_c_vp, _c_i64, _c_i64, _c_i64, _c_i64, _c_i64, _c_vp, _c_vp, _c_i64, _c_vp]),
     "w4a8_probe_stream_read": (_c_i32, [_c_vp, _c_sz, _c_vp, _c_vp]),
     "w4a8_probe_mfma_e4m3": (_c_i32, [_c_i32, _c_vp, _c_vp]),
     "w4a8_probe_mfma_flop": (ctypes.c_double, [_c_i32]),
@@ -555,6 +566,164 @@ def dpq_calibrate(w: torch.Tensor, u_factor: torch.Tensor, w_scale: torch.Tensor
                                         group_size, codes.data_ptr(), scales.data_ptr(), zeros.data_ptr(), work.data_ptr(),
                                         nbytes, _stream()), "w4a8_dpq_calibrate")
     return codes, scales, zeros
+
+
+def _rows(t: torch.Tensor, what: str, dtype: torch.dtype = torch.bfloat16):
+    """(heads, head_dim, row stride) of rows of heads, a tensor [tokens, heads, D] whose heads lie side by side."""
+    n, h, d = t.shape
+    if t.dtype != dtype or t.stride(2) != 1 or (h > 1 and t.stride(1) != d):
+        raise ValueError(f"{what}: {dtype} [tokens, heads, D] with the heads of a token side by side, got {t.dtype} {tuple(t.shape)} {t.stride()}")
+    return h, d, t.stride(0) if n > 1 else h * d
+
+
+def _flat_rows(t: torch.Tensor, n: int, width: int, dtype: torch.dtype, what: str) -> int:
+    """Row stride of a tensor [n, width]."""
+    if t.dtype != dtype or tuple(t.shape) != (n, width) or t.stride(1) != 1:
+        raise ValueError(f"{what}: {dtype} ({n}, {width}) with contiguous rows, got {t.dtype} {tuple(t.shape)} {t.stride()}")
+    return t.stride(0) if n > 1 else width
+
+
+def _cache_args(k_cache: torch.Tensor, v_cache: torch.Tensor, kv_scales: torch.Tensor | None):
+    """(element type, n_pages, page_stride, page_size, kv_heads, head_dim) of caches [pages, kv_heads, page_size, head_dim], bf16 or E4M3
+    bytes (uint8, with kv_scales)."""
+    n, hk, p, d = k_cache.shape
+    if k_cache.dtype not in (torch.bfloat16, torch.uint8) or v_cache.dtype != k_cache.dtype or v_cache.shape != k_cache.shape:
+        raise ValueError("key and value caches: both bf16 or both uint8 (E4M3 bytes), of one shape [pages, kv_heads, page_size, head_dim]")
+    for c in (k_cache, v_cache):
+        if c.stride(3) != 1 or c.stride(2) != d or (hk > 1 and c.stride(1) != p * d):
+            raise ValueError("a page of a cache is contiguous")
+    if n > 1 and k_cache.stride(0) != v_cache.stride(0):
+        raise ValueError("key and value caches have one page stride")
+    e4m3 = k_cache.dtype == torch.uint8
+    if e4m3:
+        _vector(kv_scales, torch.float32, 2, "kv_scales of an E4M3 cache")
+    return CACHE_E4M3 if e4m3 else CACHE_BF16, n, k_cache.stride(0) if n > 1 else hk * p * d, p, hk, d
+
+
+def _vector(t: torch.Tensor, dtype: torch.dtype, n: int, what: str) -> None:
+    if t is None or t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what}: {n} contiguous {dtype} values")
+
+
+def _same_device(*tensors) -> None:
+    """All of them on the current device, where the launch goes."""
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != (torch.cuda.current_device() if _current_device is None else _current_device())):
+            raise ValueError(f"a tensor on {t.device} in a call on the current device")
+
+
+def _pointer(t: torch.Tensor | None):
+    return None if t is None else t.data_ptr()
+
+
+def rope_cache_write(qkv: torch.Tensor, cos_sin: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor, k_cache: torch.Tensor,
+                     v_cache: torch.Tensor, kv_scales: torch.Tensor | None = None, rope: int = ROPE_HALVES,
+                     q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None) -> torch.Tensor:
+    """w4a8_rope_cache_write: qkv bf16 [T, (H + 2 HK) * D], cos_sin float32 [positions, D], positions and slots int32 [T], caches
+    [pages, HK, page_size, D].  Returns the rotated queries, q_out [T, H * D]; the rotated keys also go to k_out [T, HK * D] if given."""
+    dtype, n_pages, page_stride, page, hk, d = _cache_args(k_cache, v_cache, kv_scales)
+    t, width = qkv.shape
+    hq = width // d - 2 * hk
+    if width % d != 0 or hq < 1:
+        raise ValueError(f"qkv of {width} columns does not hold query heads beside {hk} key and value heads of {d} channels")
+    ld = _flat_rows(qkv, t, width, torch.bfloat16, "qkv")
+    if cos_sin.dtype != torch.float32 or cos_sin.dim() != 2 or cos_sin.shape[1] != d or not cos_sin.is_contiguous():
+        raise ValueError(f"cos_sin: contiguous float32 [positions, {d}]")
+    _vector(positions, torch.int32, t, "positions")
+    _vector(slots, torch.int32, t, "slots")
+    if q_out is None:
+        q_out = torch.empty((t, hq * d), dtype=torch.bfloat16, device=qkv.device)
+    _same_device(qkv, cos_sin, positions, slots, k_cache, v_cache, kv_scales, q_out, k_out)
+    ldq = _flat_rows(q_out, t, hq * d, torch.bfloat16, "q_out")
+    ldk = 0 if k_out is None else _flat_rows(k_out, t, hk * d, torch.bfloat16, "k_out")
+    _check(lib().w4a8_rope_cache_write(qkv.data_ptr(), t, ld, hq, hk, d, cos_sin.data_ptr(), cos_sin.shape[0], rope, positions.data_ptr(),
+                                       slots.data_ptr(), q_out.data_ptr(), ldq, _pointer(k_out), ldk, k_cache.data_ptr(), v_cache.data_ptr(),
+                                       dtype, _pointer(kv_scales), n_pages, page_stride, page, _stream()), "w4a8_rope_cache_write")
+    return q_out
+
+
+def attention_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, causal: bool = True,
+                     softmax_scale: float | None = None, out: torch.Tensor | None = None, y_scale: torch.Tensor | None = None) -> torch.Tensor:
+    """w4a8_attention_prompt: q bf16 [T, H, D], k and v [T, HK, D] (views with a row stride are fine), starts int32 [sequences + 1].
+    Returns bf16 [T, H * D], or with y_scale the E4M3 bytes (uint8) that the next layer reads.  softmax_scale: 1 / sqrt(D) if None.
+    A new output holds zeros in rows of no sequence."""
+    t = q.shape[0]
+    hq, d, ldq = _rows(q, "q")
+    hk, dk, ldk = _rows(k, "k")
+    hv, dv, ldv = _rows(v, "v")
+    if k.shape != v.shape or k.shape[0] != t or dk != d:
+        raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not belong together")
+    if starts.dim() != 1 or starts.numel() < 1:
+        raise ValueError("starts: one int32 more than there are sequences")
+    _vector(starts, torch.int32, starts.numel(), "starts")
+    dtype = torch.bfloat16 if y_scale is None else torch.uint8
+    if out is None:
+        out = torch.zeros((t, hq * d), dtype=dtype, device=q.device)
+    if y_scale is not None:
+        _vector(y_scale, torch.float32, 1, "y_scale")
+    _same_device(q, k, v, starts, out, y_scale)
+    ldy = _flat_rows(out, t, hq * d, dtype, "out")
+    _check(lib().w4a8_attention_prompt(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, starts.data_ptr(), starts.numel() - 1, t, hq,
+                                       hk, d, 1 if causal else 0, d ** -0.5 if softmax_scale is None else softmax_scale, out.data_ptr(), ldy,
+                                       _pointer(y_scale), _stream()), "w4a8_attention_prompt")
+    return out
+
+
+def attention_decode_workspace_bytes(n_seqs: int, q_heads: int, kv_heads: int, head_dim: int, page_size: int, table_width: int,
+                                     prefix_length: int = 0) -> int:
+    return lib().w4a8_attention_decode_workspace_bytes(n_seqs, q_heads, kv_heads, head_dim, page_size, table_width, prefix_length)
+
+
+def attention_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, tables: torch.Tensor, lengths: torch.Tensor,
+                     prefix_pages: torch.Tensor | None = None, prefix_length: int = 0, kv_scales: torch.Tensor | None = None,
+                     softmax_scale: float | None = None, out: torch.Tensor | None = None, y_scale: torch.Tensor | None = None,
+                     workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """w4a8_attention_decode: q bf16 [sequences, H, D], caches [pages, HK, page_size, D], tables int32 [sequences, width], lengths int32
+    [sequences], prefix_pages int32 with ceil(prefix_length / page_size) entries.  Returns bf16 [sequences, H * D], or with y_scale
+    E4M3 bytes (uint8).  workspace: uint8, attention_decode_workspace_bytes() of them; allocated here if None."""
+    n = q.shape[0]
+    hq, d, ldq = _rows(q, "q")
+    cache_dtype, n_pages, page_stride, page, hk, dk = _cache_args(k_cache, v_cache, kv_scales)
+    if dk != d or tables.dtype != torch.int32 or tables.dim() != 2 or tables.shape[0] != n or (tables.shape[1] > 1 and tables.stride(1) != 1):
+        raise ValueError(f"q {tuple(q.shape)}, cache {tuple(k_cache.shape)} and int32 tables {tuple(tables.shape)} do not belong together")
+    width = tables.shape[1]
+    _vector(lengths, torch.int32, n, "lengths")
+    if prefix_length:
+        _vector(prefix_pages, torch.int32, -(-prefix_length // page), "prefix_pages")
+    dtype = torch.bfloat16 if y_scale is None else torch.uint8
+    if out is None:
+        out = torch.empty((n, hq * d), dtype=dtype, device=q.device)
+    if y_scale is not None:
+        _vector(y_scale, torch.float32, 1, "y_scale")
+    if workspace is None:
+        need = lib().w4a8_attention_decode_workspace_bytes(n, hq, hk, d, page, width, prefix_length)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _same_device(q, k_cache, v_cache, tables, lengths, prefix_pages, kv_scales, out, y_scale, workspace)
+    ldy = _flat_rows(out, n, hq * d, dtype, "out")
+    _check(lib().w4a8_attention_decode(q.data_ptr(), ldq, n, hq, hk, d, k_cache.data_ptr(), v_cache.data_ptr(), cache_dtype, _pointer(kv_scales),
+                                       n_pages, page_stride, page, tables.data_ptr(), width, tables.stride(0) if n > 1 else width,
+                                       lengths.data_ptr(), _pointer(prefix_pages), prefix_length,
+                                       d ** -0.5 if softmax_scale is None else softmax_scale, out.data_ptr(), ldy, _pointer(y_scale),
+                                       _pointer(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                       _stream()), "w4a8_attention_decode")
+    return out
+
+
+def cache_copy_pages(cache: torch.Tensor, src: torch.Tensor, dst: torch.Tensor) -> torch.Tensor:
+    """w4a8_cache_copy_pages: cache [planes, pages, ...] of any type, pages contiguous; pages src (int32) -> dst in every plane."""
+    planes, pages = cache.shape[:2]
+    if pages < 1 or cache.numel() == 0 or not cache[0, 0].is_contiguous():
+        raise ValueError("cache: [planes, pages, ...] with contiguous pages")
+    size = cache.element_size()
+    _vector(src, torch.int32, src.numel(), "src")
+    _vector(dst, torch.int32, src.numel(), "dst")
+    _same_device(cache, src, dst)
+    page_bytes = cache[0, 0].numel() * size
+    _check(lib().w4a8_cache_copy_pages(cache.data_ptr(), planes, cache.stride(0) * size if planes > 1 else 0, pages,
+                                       cache.stride(1) * size if pages > 1 else page_bytes, page_bytes, src.data_ptr(), dst.data_ptr(),
+                                       src.numel(), _stream()), "w4a8_cache_copy_pages")
+    return cache
 
 
 def probe_stream_read(buf: torch.Tensor, sink: torch.Tensor) -> None:

@@ -1,0 +1,64 @@
+// Device-side helpers of the attention kernels (gfx950 only).
+#pragma once
+#include "w4a8_device.hpp"
+
+namespace w4a8 {
+
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+
+constexpr float NEG_INF = -__builtin_huge_valf();
+
+__device__ __forceinline__ v4f mfma_16x16x32_bf16(v8bf a, v8bf b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ v16f mfma_32x32x16_bf16(v8bf a, v8bf b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Two float32 -> two bf16 (round to nearest even), `a` in the low half: one instruction.
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    v2bf r;
+    r[0] = (__bf16)a;
+    r[1] = (__bf16)b;
+    return __builtin_bit_cast(uint32_t, r);
+}
+// The two E4M3 bytes in the low (HIGH: high) half of w as bf16, exactly.
+template <bool HIGH> __device__ __forceinline__ uint32_t e4m3_to_bf16(uint32_t w) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HIGH));
+}
+
+// x of this lane against that of the lane 32 (16) away, in both.
+__device__ __forceinline__ float max_over_32(float x) {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ __forceinline__ float max_over_16(float x) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ __forceinline__ float sum_over_32(float x) {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+__device__ __forceinline__ float sum_over_16(float x) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+
+// 1 / sum of a finished row; a row that saw nothing (sum 0) gives zeros.
+__device__ __forceinline__ float inverse_sum(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+
+// Four finished channels of a row, to 8 bytes of bf16 or to 4 E4M3 bytes.  The E4M3 bytes are those of the bf16 values, so that they
+// are the bytes that the activation quantization makes of a bf16 output.
+__device__ __forceinline__ void store_4(uint16_t* p, float a, float b, float c, float d, const StaticQuantizer&) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
+}
+__device__ __forceinline__ void store_4(uint8_t* p, float a, float b, float c, float d, const StaticQuantizer& q) {
+    const uint32_t lo = pack_bf16(a, b), hi = pack_bf16(c, d);
+    *reinterpret_cast<uint32_t*>(p) = q.four(__uint_as_float(lo << 16), __uint_as_float(lo & 0xFFFF0000u), __uint_as_float(hi << 16),
+                                             __uint_as_float(hi & 0xFFFF0000u));
+}
+
+}  // namespace w4a8

@@ -1,0 +1,287 @@
+// Attention inside whole prompts: packed sequences, grouped heads, causal or both ways.
+//   o_i = sum_j softmax_j(q_i . k_j * scale) v_j,   j in i's sequence, j <= i if causal
+// One pass over the keys with a running maximum and sum per row: a workgroup owns 32 rows per wavefront of one query head and walks the
+// sequence's keys 64 at a time.  Both products are formed transposed, S^T = K Q^T and O^T = V^T P^T: a lane then holds one row's
+// scores, its maximum is found in registers (and one exchange with the lane 32 away), and the 16 keys whose scores a lane has
+// are, in the same order, those of the second product's operand: P never leaves the registers.  Keys and values come to LDS by
+// copies that pass no registers, one tile ahead; V^T is read from it by transposing reads.
+#include "attention.hpp"
+#include "attention_device.hpp"
+
+namespace w4a8 {
+namespace {
+
+constexpr int XCDS_A = 8;
+constexpr int BN = 64;                                           // keys per tile
+
+// LDS keeps rows of D bf16 in 16-byte pieces, piece p of row r at p ^ swizzle(r): eight rows next to each other have any one piece in
+// eight different bank groups (the rows a read of K touches), and four rows' 64-byte quarters lie in four (a transposing read of V).
+template <int D> __device__ __forceinline__ constexpr int swizzle(int r) {
+    return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+}
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// The sequence and, counted from its end, the tile of rows of unit t (0 .. tiles - 1) of the packed batch; false behind the last.
+template <int BM>
+__device__ __forceinline__ bool find_tile(const int32_t* starts, int n_seqs, int64_t T, int t, int& seq_start, int& len, int& tile) {
+    const int lane = threadIdx.x & 63;
+    for (int base = 0; base < n_seqs; base += 64) {
+        const int s = base + lane;
+        int b = 0, n = 0;
+        if (s < n_seqs) {
+            const int64_t lo = starts[s] < 0 ? 0 : starts[s], hi = starts[s + 1] < T ? starts[s + 1] : T;
+            b = (int)lo;
+            n = hi > lo ? (int)(hi - lo) : 0;
+        }
+        const int mine = (n + BM - 1) / BM;
+        int upto = mine;                                         // tiles of this sequence and of those before it
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int other = __shfl_up(upto, d);
+            if (lane >= d) upto += other;
+        }
+        const uint64_t here = __builtin_amdgcn_ballot_w64(t < upto);
+        if (here) {
+            const int first = __builtin_ctzll(here);
+            seq_start = __builtin_amdgcn_readlane(b, first);
+            len = __builtin_amdgcn_readlane(n, first);
+            tile = __builtin_amdgcn_readlane(upto, first) - 1 - t;
+            return true;
+        }
+        t -= __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
+
+template <int D, int WAVES, bool CAUSAL, typename OutT>
+__global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptArgs a, int tiles, int by_head) {
+    constexpr int BM = 32 * WAVES, ROW = 2 * D, PIECES = D / 8, TILE = BN * ROW;
+    constexpr int COPIES = TILE / 1024 / WAVES;                  // of 64 lanes x 16 bytes, per wavefront for each of K and V
+    constexpr int KS = D / 16, DT = D / 32, KT = BN / 32;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * TILE];   // K 0, K 1, V 0, V 1
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const int group = a.q_heads / a.kv_heads;
+
+    // by_head: every XCD keeps to its own key heads, whose keys and values then stay in its L2; a tile's query heads that share a
+    // key head run side by side.
+    int t, head;
+    if (by_head) {
+        const int x = blockIdx.x % XCDS_A, i = blockIdx.x / XCDS_A;
+        const int heads_x = a.kv_heads / XCDS_A * group;
+        t = i / heads_x;
+        const int h = i - t * heads_x;
+        head = (h / group * XCDS_A + x) * group + h % group;
+    } else {
+        t = blockIdx.x / a.q_heads;
+        head = blockIdx.x - t * a.q_heads;
+    }
+    const int kv_head = head / group;
+    int seq_start, len, tile;
+    if (!find_tile<BM>(a.starts, a.n_seqs, a.T, t, seq_start, len, tile)) return;
+    const int q0 = tile * BM, row = q0 + 32 * wave + col;        // this lane's row of the sequence
+    const int key_end = CAUSAL ? min(len, q0 + BM) : len;
+    const int n_tiles = (key_end + BN - 1) / BN;
+
+    // Q^T, the second operand of S^T = K Q^T, for the whole walk
+    v8bf qf[KS];
+    {
+        const uint16_t* qrow = a.q + (int64_t)(seq_start + min(row, len - 1)) * a.ldq + (int64_t)head * D + 8 * half;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const v8bf*>(qrow + 16 * s);
+    }
+    const uint8_t* kbase = reinterpret_cast<const uint8_t*>(a.k + (int64_t)seq_start * a.ldk + (int64_t)kv_head * D);
+    const uint8_t* vbase = reinterpret_cast<const uint8_t*>(a.v + (int64_t)seq_start * a.ldv + (int64_t)kv_head * D);
+    constexpr int RPC = 1024 / ROW;                              // rows per copy
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+    auto copy_tile = [&](int kt, int buffer) {
+        const uint8_t* kt_base = kbase + (int64_t)kt * BN * a.ldk * 2;
+        const uint8_t* vt_base = vbase + (int64_t)kt * BN * a.ldv * 2;
+        const int last = len - 1 - kt * BN;
+#pragma unroll
+        for (int q = 0; q < COPIES; ++q) {
+            const int n = wave * COPIES + q;
+            const int r = n * RPC + lane / PIECES, from = min(r, last);
+            const uint32_t piece = (uint32_t)(((lane % PIECES) ^ swizzle<D>(r)) * 16);
+            lds_dma_16(kt_base, (uint32_t)(from * (int)(a.ldk * 2)) + piece, lds_base + buffer * TILE + n * 1024);
+            lds_dma_16(vt_base, (uint32_t)(from * (int)(a.ldv * 2)) + piece, lds_base + (2 + buffer) * TILE + n * 1024);
+        }
+    };
+    // LDS addresses: K operand of step s: piece 2s + half of row col (+ 32 kt).  V^T operand (step t of 16 keys, channels 32 dt ..): keys
+    // 16t + 4 half + {0..3} and 8 more, 16 channels per 16 lanes
+    const uint32_t k_addr = lds_base + col * ROW, k_piece = (uint32_t)(half ^ swizzle<D>(col));
+    const int j = lane & 15, g1 = (lane >> 4) & 1;
+    const uint32_t v_row = (uint32_t)((4 * half + (j >> 2)) * ROW), v_piece = (uint32_t)((2 * g1 + ((j & 3) >> 1)) ^ swizzle<D>(4 * half + (j >> 2)));
+    const uint32_t v_addr = lds_base + 2 * TILE + v_row + (j & 1) * 8;
+
+    // A weight of zero takes a key out of the sums, unless its value is no number.  So a walk that ends with an output that is none is
+    // walked again carefully: there, in tiles that hide keys from some rows, values that are no numbers enter only the rows that see them.
+    v16f o[DT];
+    float m, l;                                                  // maximum of the scores so far (scaled, base 2), this lane's part of the sum
+    auto walk = [&](auto careful) {
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
+    m = NEG_INF;
+    l = 0.0f;
+    copy_tile(0, 0);
+    for (int kt = 0; kt < n_tiles; ++kt) {
+        const int buffer = kt & 1;
+        lds_dma_wait_all();
+        __syncthreads();
+        if (kt + 1 < n_tiles) copy_tile(kt + 1, buffer ^ 1);
+        const int key0 = kt * BN;
+        if (CAUSAL && key0 > q0 + 32 * wave + 31) continue;      // (wave-uniform) no row of this wavefront sees the tile
+        v16f s[KT];
+#pragma unroll
+        for (int k = 0; k < KT; ++k) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[k][r] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                const uint32_t at = k_addr + buffer * TILE + k * 32 * ROW + ((k_piece ^ (2 * i)) << 4);
+                const v8bf kf = *reinterpret_cast<__attribute__((address_space(3))) const v8bf*>((uintptr_t)at);
+                s[k] = mfma_32x32x16_bf16(kf, qf[i], s[k]);
+            }
+        }
+        const bool masked = key0 + BN > len || (CAUSAL && key0 + BN - 1 > q0 + 32 * wave);
+        const int seen = CAUSAL ? min(len, row + 1) : len;       // keys below this one
+        if (masked) {
+#pragma unroll
+            for (int k = 0; k < KT; ++k)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (key0 + 32 * k + (r & 3) + 8 * (r >> 2) + 4 * half >= seen) s[k][r] = NEG_INF;
+        }
+        float mx = s[0][0];
+#pragma unroll
+        for (int k = 0; k < KT; ++k)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[k][r]);
+        mx = max_over_32(mx) * a.scale_log2;
+        const float m_new = fmaxf(m, mx);
+        const float m_use = m_new == NEG_INF ? 0.0f : m_new;
+        if (__builtin_amdgcn_ballot_w64(m_new > m)) {
+            const float alpha = exp2_fast(m - m_use);
+            l *= alpha;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
+            m = m_new;
+        }
+        uint32_t p[KT][8];
+#pragma unroll
+        for (int k = 0; k < KT; ++k)
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) {
+                const float p0 = exp2_fast(fmaf(s[k][r], a.scale_log2, -m_use)), p1 = exp2_fast(fmaf(s[k][r + 1], a.scale_log2, -m_use));
+                l += p0 + p1;
+                p[k][r / 2] = pack_bf16(p0, p1);
+            }
+        auto v_operand = [&](int t16, int d) {
+            const uint32_t at = v_addr + buffer * TILE + t16 * 16 * ROW;
+            union {
+                v4s part[2];
+                u32x4 whole;
+            } vf;
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                vf.part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)(
+                    at + e * 8 * ROW + ((v_piece ^ (4 * d) ^ (2 * e)) << 4)));
+            return vf.whole;
+        };
+        if (careful.value && masked) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll 1
+                for (int sign = 0; sign < 2; ++sign) {           // +infinity and NaN, then -infinity and NaN
+                    v16f count;                                  // of such values that the row sees
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) count[r] = 0.0f;
+#pragma unroll
+                    for (int t16 = 0; t16 < BN / 16; ++t16) {
+                        int open_to = seen;
+                        asm volatile("" : "+v"(open_to));        // formed here each time: registers are short, time is not
+                        __builtin_amdgcn_sched_barrier(0);
+                        u32x4 v = v_operand(t16, d), found, sees;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t number = 0, hit = 0, open = 0;
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) {
+                                const uint32_t x = (v[i] >> (16 * u)) & 0xFFFFu;
+                                const bool none = (x & 0x7F80u) == 0x7F80u, nan = none && (x & 0x7Fu);
+                                const int e = 2 * i + u;
+                                if (!none) number |= x << (16 * u);
+                                if (nan || (none && (x >> 15) == (uint32_t)sign)) hit |= 0x3F80u << (16 * u);
+                                if (key0 + 16 * t16 + (e & 3) + 8 * (e >> 2) + 4 * half < open_to) open |= 0x3F80u << (16 * u);
+                            }
+                            v[i] = number;
+                            found[i] = hit;
+                            sees[i] = open;
+                        }
+                        const uint32_t* pk = p[t16 / 2] + 4 * (t16 & 1);
+                        if (sign == 0)
+                            o[d] = mfma_32x32x16_bf16(__builtin_bit_cast(v8bf, v), __builtin_bit_cast(v8bf, u32x4{pk[0], pk[1], pk[2], pk[3]}), o[d]);
+                        count = mfma_32x32x16_bf16(__builtin_bit_cast(v8bf, found), __builtin_bit_cast(v8bf, sees), count);
+                    }
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (count[r] > 0.0f) o[d][r] += sign ? NEG_INF : -NEG_INF;
+                }
+            continue;
+        }
+#pragma unroll
+        for (int t16 = 0; t16 < BN / 16; ++t16) {
+            const uint32_t* pk = p[t16 / 2] + 4 * (t16 & 1);
+            const v8bf pf = __builtin_bit_cast(v8bf, u32x4{pk[0], pk[1], pk[2], pk[3]});
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] = mfma_32x32x16_bf16(__builtin_bit_cast(v8bf, v_operand(t16, d)), pf, o[d]);
+        }
+    }
+    };
+    walk(std::false_type{});
+    float none = 0.0f;                                           // NaN if any output is no number
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) none = fmaf(o[d][r], 0.0f, none);
+    if (__builtin_expect(__syncthreads_or(none != 0.0f), 0)) walk(std::true_type{});
+    const float inv = inverse_sum(sum_over_32(l));
+    if (row < len) {
+        const StaticQuantizer quant(a.y_scale ? *a.y_scale : 1.0f);
+        OutT* y = static_cast<OutT*>(a.y) + (int64_t)(seq_start + row) * a.ldy + (int64_t)head * D;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                store_4(y + 32 * d + 8 * (r >> 2) + 4 * half, o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv, quant);
+    }
+}
+
+template <int D, int WAVES, bool CAUSAL>
+void launch_tile(const PromptArgs& a, hipStream_t st) {
+    const int64_t tiles = a.T / (32 * WAVES) + a.n_seqs;         // at most
+    const int by_head = a.kv_heads % XCDS_A == 0;
+    const dim3 grid((unsigned)(tiles * a.q_heads)), block(64 * WAVES);
+    if (a.y_scale) hipLaunchKernelGGL((attention_prompt_kernel<D, WAVES, CAUSAL, uint8_t>), grid, block, 0, st, a, (int)tiles, by_head);
+    else hipLaunchKernelGGL((attention_prompt_kernel<D, WAVES, CAUSAL, uint16_t>), grid, block, 0, st, a, (int)tiles, by_head);
+}
+
+}  // namespace
+
+int launch_attention_prompt(const PromptArgs& a, hipStream_t st) {
+    if (a.head_dim == 128) {
+        if (a.causal) launch_tile<128, 4, true>(a, st);
+        else launch_tile<128, 4, false>(a, st);
+    } else {
+        if (a.causal) launch_tile<64, 4, true>(a, st);
+        else launch_tile<64, 4, false>(a, st);
+    }
+    return launch_status();
+}
+
+}  // namespace w4a8
