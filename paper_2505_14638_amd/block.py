@@ -11,6 +11,9 @@ it (w4a8_linear_fp8_out for QKV and O, w4a8_linear_silu_mul_fp8_out for gate|up 
 copy of the gate|up weights) and, up to eight tokens, the quantization of the block input folded into the QKV layer
 (w4a8_linear_quantize_in_fp8_out): four or five launches instead of nine, the same bytes at every layer input and the
 same block output.
+
+`DecoderBlock` has attention in that place: queries and keys are rotated, keys and values go to a paged cache, and whole prompts or single
+tokens of a batch attend; with `fused=True` attention writes the E4M3 bytes that the O projection reads.
 """
 from __future__ import annotations
 
@@ -86,14 +89,21 @@ class DecoderBlockLinears:
         else:
             B.quantize_act(x, sx["qkv"], out=x8)
             B.linear_fp8_out(x8, sx["qkv"], *w["qkv"], self.dims["qkv"][1], g, sx["o"], out=qkv8)
-        o8 = B.linear_fp8_out(qkv8[:, :self.hidden], sx["o"], *w["o"], self.hidden, g, sx["gate_up"],
+        if keep is not None:
+            keep.update(qkv_x8=x8, o_x8=qkv8[:, :self.hidden])
+        return self._from_o_fused(qkv8[:, :self.hidden], m, keep)
+
+    def _from_o_fused(self, o_x8: torch.Tensor, m: int, keep: dict | None) -> torch.Tensor:
+        """The O projection's E4M3 input to the block's output."""
+        g, sx, w = self.group_size, self.scales_x, self.weights
+        o8 = B.linear_fp8_out(o_x8, sx["o"], *w["o"], self.hidden, g, sx["gate_up"],
                               out=self._buf(("o", "y8", m), (m, self.hidden), torch.uint8))
         h8 = self._buf(("h8", m), (m, self.ffn), torch.uint8)
         B.linear_silu_mul_fp8_out(o8, sx["gate_up"], *w["gate_up_interleaved"], self.ffn, g, sx["down"], out=h8)
         y = B.linear(h8, sx["down"], *w["down"], self.hidden, g, B.LAYOUT_TILED,
                      out=self._buf(("down", "y", m), (m, self.hidden), torch.bfloat16), workspace=self._ws("down", m))
         if keep is not None:
-            keep.update(qkv_x8=x8, o_x8=qkv8[:, :self.hidden], gate_up_x8=o8, down_x8=h8, down=y)
+            keep.update(gate_up_x8=o8, down_x8=h8, down=y)
         return y
 
     def forward(self, x: torch.Tensor, keep: dict | None = None) -> torch.Tensor:
@@ -102,11 +112,84 @@ class DecoderBlockLinears:
             return self._forward_fused(x, keep)
         m = x.shape[0]
         qkv = self._linear("qkv", x, m)
-        o = self._linear("o", qkv[:, :self.hidden], m)
+        y = self._from_o(qkv[:, :self.hidden], m, keep)
+        if keep is not None:
+            keep.update(qkv=qkv, qkv_x8=self._buffers[("qkv", "x8", m)])
+        return y
+
+    def _from_o(self, attended: torch.Tensor, m: int, keep: dict | None) -> torch.Tensor:
+        """The O projection's bf16 input to the block's output."""
+        o = self._linear("o", attended, m)
         gu = self._linear("gate_up", o, m)
         h = B.silu_mul(gu, out=self._buf(("h", m), (m, self.ffn), torch.bfloat16))
         y = self._linear("down", h, m)
         if keep is not None:
-            keep.update(qkv=qkv, o=o, gate_up=gu, h=h, down=y,
-                        **{nm + "_x8": self._buffers[(nm, "x8", m)] for nm in LAYERS})
+            keep.update(o=o, gate_up=gu, h=h, down=y, **{nm + "_x8": self._buffers[(nm, "x8", m)] for nm in LAYERS[1:]})
         return y
+
+
+class DecoderBlock(DecoderBlockLinears):
+    """A block with attention between QKV and O: `heads` query heads and `kv_heads` key and value heads of hidden / heads channels."""
+
+    def __init__(self, hidden: int, ffn: int, heads: int, kv_heads: int, cos_sin: torch.Tensor, rope: int = B.ROPE_HALVES,
+                 group_size: int = 128, device: str = "cuda:0", fused: bool = False):
+        """cos_sin: float32 [positions, head_dim], the table of w4a8_rope_cache_write (rotary_table makes one)."""
+        if hidden % heads != 0 or heads % kv_heads != 0:
+            raise ValueError(f"hidden {hidden}, heads {heads}, kv_heads {kv_heads} do not divide")
+        self.heads, self.kv_heads, self.head_dim, self.cos_sin, self.rope = heads, kv_heads, hidden // heads, cos_sin, rope
+        super().__init__(hidden, ffn, hidden + 2 * kv_heads * self.head_dim, group_size, device, fused)
+
+    def forward(self, x: torch.Tensor, keep: dict | None = None) -> torch.Tensor:
+        raise TypeError("attention needs to know what x is: forward_prompt or forward_decode")
+
+    def _qkv(self, x: torch.Tensor, m: int, keep: dict | None) -> torch.Tensor:
+        if self.fused and m <= self.quantize_in_up_to and m * self.hidden <= 65536:
+            return B.linear_quantize_in(x, self.scales_x["qkv"], *self.weights["qkv"], self.dims["qkv"][1], self.group_size,
+                                        out=self._buf(("qkv", "y", m), (m, self.dims["qkv"][1]), torch.bfloat16),
+                                        x8_out=self._buf(("qkv", "x8", m), (m, self.hidden), torch.uint8) if keep is not None else None)
+        return self._linear("qkv", x, m)
+
+    def _rows(self, name: str, m: int, heads: int) -> torch.Tensor:
+        return self._buf((name, m), (m, heads * self.head_dim), torch.bfloat16)
+
+    def _attended(self, m: int):
+        """(output of attention, its scale): E4M3 for the O projection where the quantization is folded in."""
+        if self.fused:
+            return self._buf(("o", "x8", m), (m, self.hidden), torch.uint8), self.scales_x["o"]
+        return self._rows("attended", m, self.heads), None
+
+    def _finish(self, out: torch.Tensor, qkv: torch.Tensor, m: int, keep: dict | None) -> torch.Tensor:
+        if keep is not None:
+            keep.update(qkv=qkv, qkv_x8=self._buffers[("qkv", "x8", m)], **({"o_x8": out} if self.fused else {"attended": out}))
+        return self._from_o_fused(out, m, keep) if self.fused else self._from_o(out, m, keep)
+
+    def forward_prompt(self, x: torch.Tensor, starts: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor, cache,
+                       keep: dict | None = None) -> torch.Tensor:
+        """Whole prompts, packed: x bf16 [M, hidden], starts int32 [sequences + 1] (rows of no sequence get what their buffer held);
+        positions and slots int32 [M], where each token goes in `cache` = (keys, values, scales or None)."""
+        m, (k_cache, v_cache, kv_scales) = x.shape[0], cache
+        qkv = self._qkv(x, m, keep)
+        q, k = self._rows("q", m, self.heads), self._rows("k", m, self.kv_heads)
+        B.rope_cache_write(qkv, self.cos_sin, positions, slots, k_cache, v_cache, kv_scales, self.rope, q_out=q, k_out=k)
+        out, y_scale = self._attended(m)
+        shape = (self.kv_heads, self.head_dim)
+        B.attention_prompt(q.view(m, self.heads, self.head_dim), k.view(m, *shape), qkv[:, -self.kv_heads * self.head_dim:].unflatten(1, shape),
+                           starts, out=out, y_scale=y_scale)
+        return self._finish(out, qkv, m, keep)
+
+    def forward_decode(self, x: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor, cache, tables: torch.Tensor, lengths: torch.Tensor,
+                       prefix_pages: torch.Tensor | None = None, prefix_length: int = 0, keep: dict | None = None) -> torch.Tensor:
+        """One token of each sequence: x bf16 [M, hidden]; its keys and values go to `slots` first, so `lengths` count it."""
+        m, (k_cache, v_cache, kv_scales) = x.shape[0], cache
+        qkv = self._qkv(x, m, keep)
+        q = B.rope_cache_write(qkv, self.cos_sin, positions, slots, k_cache, v_cache, kv_scales, self.rope, q_out=self._rows("q", m, self.heads))
+        out, y_scale = self._attended(m)
+        B.attention_decode(q.view(m, self.heads, self.head_dim), k_cache, v_cache, tables, lengths, prefix_pages, prefix_length, kv_scales,
+                           out=out, y_scale=y_scale)
+        return self._finish(out, qkv, m, keep)
+
+
+def rotary_table(positions: int, head_dim: int, base: float = 10000.0, device: str = "cuda:0") -> torch.Tensor:
+    """float32 [positions, head_dim]: cosines, then sines of position * base^(-2i / head_dim), the angles in 64 bits."""
+    angle = torch.arange(positions, dtype=torch.float64)[:, None] * base ** (-torch.arange(0, head_dim, 2, dtype=torch.float64) / head_dim)
+    return torch.cat([angle.cos(), angle.sin()], dim=1).float().to(device)
