@@ -47,18 +47,29 @@ __device__ __forceinline__ float sum_over_16(float x) {
     return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
+// Sum of the two bf16 in w, added to c.
+__device__ __forceinline__ float add_pair(uint32_t w, float c) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, w), __builtin_bit_cast(v2bf, 0x3F803F80u), c, false);
+}
+
+// A row's weights are 2^(score - m) with m a maximum of earlier scores: it follows a new one only when that is over 2^RISE times as
+// large, so that the sums are seldom scaled again.  Weights up to 2^RISE lose nothing in float32 or bf16.
+constexpr float RISE = 8.0f;
+
 // 1 / sum of a finished row; a row that saw nothing (sum 0) gives zeros.
 __device__ __forceinline__ float inverse_sum(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 
-// Four finished channels of a row, to 8 bytes of bf16 or to 4 E4M3 bytes.  The E4M3 bytes are those of the bf16 values, so that they
-// are the bytes that the activation quantization makes of a bf16 output.
+// Four bf16 (two in each word) to four E4M3 bytes, those that the activation quantization makes of them.
+__device__ __forceinline__ uint32_t quant_bf16(uint32_t lo, uint32_t hi, const StaticQuantizer& q) {
+    return q.four(__uint_as_float(lo << 16), __uint_as_float(lo & 0xFFFF0000u), __uint_as_float(hi << 16), __uint_as_float(hi & 0xFFFF0000u));
+}
+
+// Four finished channels of a row, to 8 bytes of bf16 or to 4 E4M3 bytes of those bf16 values.
 __device__ __forceinline__ void store_4(uint16_t* p, float a, float b, float c, float d, const StaticQuantizer&) {
     *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
 }
 __device__ __forceinline__ void store_4(uint8_t* p, float a, float b, float c, float d, const StaticQuantizer& q) {
-    const uint32_t lo = pack_bf16(a, b), hi = pack_bf16(c, d);
-    *reinterpret_cast<uint32_t*>(p) = q.four(__uint_as_float(lo << 16), __uint_as_float(lo & 0xFFFF0000u), __uint_as_float(hi << 16),
-                                             __uint_as_float(hi & 0xFFFF0000u));
+    *reinterpret_cast<uint32_t*>(p) = quant_bf16(pack_bf16(a, b), pack_bf16(c, d), q);
 }
 
 }  // namespace w4a8

@@ -59,7 +59,8 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
     constexpr int BM = 32 * WAVES, ROW = 2 * D, PIECES = D / 8, TILE = BN * ROW;
     constexpr int COPIES = TILE / 1024 / WAVES;                  // of 64 lanes x 16 bytes, per wavefront for each of K and V
     constexpr int KS = D / 16, DT = D / 32, KT = BN / 32;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * TILE];   // K 0, K 1, V 0, V 1
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * TILE];   // K 0, V 0, K 1, V 1; first Q, in K 1 and V 1; at last O, in K 0 and V 0
+    static_assert(BM * ROW <= 2 * TILE, "Q and O fit two tiles");
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
     const int group = a.q_heads / a.kv_heads;
@@ -84,36 +85,68 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
     const int key_end = CAUSAL ? min(len, q0 + BM) : len;
     const int n_tiles = (key_end + BN - 1) / BN;
 
-    // Q^T, the second operand of S^T = K Q^T, for the whole walk
-    v8bf qf[KS];
-    {
-        const uint16_t* qrow = a.q + (int64_t)(seq_start + min(row, len - 1)) * a.ldq + (int64_t)head * D + 8 * half;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const v8bf*>(qrow + 16 * s);
-    }
     const uint8_t* kbase = reinterpret_cast<const uint8_t*>(a.k + (int64_t)seq_start * a.ldk + (int64_t)kv_head * D);
     const uint8_t* vbase = reinterpret_cast<const uint8_t*>(a.v + (int64_t)seq_start * a.ldv + (int64_t)kv_head * D);
     constexpr int RPC = 1024 / ROW;                              // rows per copy
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+    uint32_t k_from[COPIES], v_from[COPIES];                     // where this lane's 16 bytes of its copies come from, within a tile
+#pragma unroll
+    for (int q = 0; q < COPIES; ++q) {
+        const int r = (wave * COPIES + q) * RPC + lane / PIECES;
+        const uint32_t piece = (uint32_t)(((lane % PIECES) ^ swizzle<D>(r)) * 16);
+        k_from[q] = (uint32_t)r * (uint32_t)(a.ldk * 2) + piece;
+        v_from[q] = (uint32_t)r * (uint32_t)(a.ldv * 2) + piece;
+    }
     auto copy_tile = [&](int kt, int buffer) {
         const uint8_t* kt_base = kbase + (int64_t)kt * BN * a.ldk * 2;
         const uint8_t* vt_base = vbase + (int64_t)kt * BN * a.ldv * 2;
-        const int last = len - 1 - kt * BN;
+        const uint32_t to = lds_base + 2 * buffer * TILE + wave * COPIES * 1024;
+        const int left = len - kt * BN;                          // rows behind the sequence's last one are that one
+        if (left >= BN) {
 #pragma unroll
-        for (int q = 0; q < COPIES; ++q) {
-            const int n = wave * COPIES + q;
-            const int r = n * RPC + lane / PIECES, from = min(r, last);
-            const uint32_t piece = (uint32_t)(((lane % PIECES) ^ swizzle<D>(r)) * 16);
-            lds_dma_16(kt_base, (uint32_t)(from * (int)(a.ldk * 2)) + piece, lds_base + buffer * TILE + n * 1024);
-            lds_dma_16(vt_base, (uint32_t)(from * (int)(a.ldv * 2)) + piece, lds_base + (2 + buffer) * TILE + n * 1024);
+            for (int q = 0; q < COPIES; ++q) {
+                lds_dma_16(kt_base, k_from[q], to + q * 1024);
+                lds_dma_16(vt_base, v_from[q], to + TILE + q * 1024);
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < COPIES; ++q) {
+                const int r = (wave * COPIES + q) * RPC + lane / PIECES;
+                const uint32_t back = r < left ? 0u : (uint32_t)(r - left + 1);
+                lds_dma_16(kt_base, k_from[q] - back * (uint32_t)(a.ldk * 2), to + q * 1024);
+                lds_dma_16(vt_base, v_from[q] - back * (uint32_t)(a.ldv * 2), to + TILE + q * 1024);
+            }
         }
     };
     // LDS addresses: K operand of step s: piece 2s + half of row col (+ 32 kt).  V^T operand (step t of 16 keys, channels 32 dt ..): keys
     // 16t + 4 half + {0..3} and 8 more, 16 channels per 16 lanes
-    const uint32_t k_addr = lds_base + col * ROW, k_piece = (uint32_t)(half ^ swizzle<D>(col));
+    uint32_t k_addr[KS], v_addr[DT][2];
+#pragma unroll
+    for (int i = 0; i < KS; ++i) k_addr[i] = lds_base + col * ROW + (uint32_t)(((half ^ swizzle<D>(col)) ^ (2 * i)) << 4);
     const int j = lane & 15, g1 = (lane >> 4) & 1;
-    const uint32_t v_row = (uint32_t)((4 * half + (j >> 2)) * ROW), v_piece = (uint32_t)((2 * g1 + ((j & 3) >> 1)) ^ swizzle<D>(4 * half + (j >> 2)));
-    const uint32_t v_addr = lds_base + 2 * TILE + v_row + (j & 1) * 8;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = 4 * half + (j >> 2), piece = 2 * g1 + ((j & 3) >> 1);
+            v_addr[d][e] = lds_base + TILE + (r + 8 * e) * ROW + (j & 1) * 8 + (uint32_t)((piece ^ swizzle<D>(r) ^ (4 * d) ^ (2 * e)) << 4);
+        }
+
+    // Q^T, the second operand of S^T = K Q^T, stays in registers; it comes through LDS, since whole rows are what memory gives fast
+    v8bf qf[KS];
+    {
+        const uint8_t* rows = reinterpret_cast<const uint8_t*>(a.q + (int64_t)(seq_start + q0) * a.ldq + (int64_t)head * D);
+#pragma unroll
+        for (int q = 0; q < 32 / RPC; ++q) {
+            const int r = 32 * wave + q * RPC + lane / PIECES;
+            lds_dma_16(rows, (uint32_t)min(r, len - 1 - q0) * (uint32_t)(a.ldq * 2) + (uint32_t)(((lane % PIECES) ^ swizzle<D>(r)) * 16),
+                       lds_base + 2 * TILE + (32 * wave + q * RPC) * ROW);
+        }
+        lds_dma_wait_all();                                      // a wavefront copies its own rows
+#pragma unroll
+        for (int i = 0; i < KS; ++i)
+            qf[i] = *reinterpret_cast<__attribute__((address_space(3))) const v8bf*>((uintptr_t)(k_addr[i] + 2 * TILE + wave * 32 * ROW));
+    }
 
     // A weight of zero takes a key out of the sums, unless its value is no number.  So a walk that ends with an output that is none is
     // walked again carefully: there, in tiles that hide keys from some rows, values that are no numbers enter only the rows that see them.
@@ -127,13 +160,13 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
     m = NEG_INF;
     l = 0.0f;
     copy_tile(0, 0);
-    for (int kt = 0; kt < n_tiles; ++kt) {
-        const int buffer = kt & 1;
+    auto step = [&](int kt, auto buffer_c) {
+        constexpr int buffer = decltype(buffer_c)::value;
         lds_dma_wait_all();
         __syncthreads();
         if (kt + 1 < n_tiles) copy_tile(kt + 1, buffer ^ 1);
         const int key0 = kt * BN;
-        if (CAUSAL && key0 > q0 + 32 * wave + 31) continue;      // (wave-uniform) no row of this wavefront sees the tile
+        if (CAUSAL && key0 > q0 + 32 * wave + 31) return;        // (wave-uniform) no row of this wavefront sees the tile
         v16f s[KT];
 #pragma unroll
         for (int k = 0; k < KT; ++k) {
@@ -141,19 +174,23 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
             for (int r = 0; r < 16; ++r) s[k][r] = 0.0f;
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
-                const uint32_t at = k_addr + buffer * TILE + k * 32 * ROW + ((k_piece ^ (2 * i)) << 4);
-                const v8bf kf = *reinterpret_cast<__attribute__((address_space(3))) const v8bf*>((uintptr_t)at);
+                const v8bf kf = *reinterpret_cast<__attribute__((address_space(3))) const v8bf*>((uintptr_t)(k_addr[i] + 2 * buffer * TILE + k * 32 * ROW));
                 s[k] = mfma_32x32x16_bf16(kf, qf[i], s[k]);
             }
         }
         const bool masked = key0 + BN > len || (CAUSAL && key0 + BN - 1 > q0 + 32 * wave);
         const int seen = CAUSAL ? min(len, row + 1) : len;       // keys below this one
-        if (masked) {
+        // a loop of at most one pass: as a branch the compiler turns it into 32 comparisons and selects in every tile
+        int hides = uniform(masked);
+        while (hides) {
+            int edge = seen - key0 - 4 * half;
+            asm volatile("" : "+v"(edge));
 #pragma unroll
             for (int k = 0; k < KT; ++k)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (key0 + 32 * k + (r & 3) + 8 * (r >> 2) + 4 * half >= seen) s[k][r] = NEG_INF;
+                    if (32 * k + (r & 3) + 8 * (r >> 2) >= edge) s[k][r] = NEG_INF;
+            asm volatile("s_mov_b32 %0, 0" : "=s"(hides));
         }
         float mx = s[0][0];
 #pragma unroll
@@ -161,10 +198,8 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
 #pragma unroll
             for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[k][r]);
         mx = max_over_32(mx) * a.scale_log2;
-        const float m_new = fmaxf(m, mx);
-        const float m_use = m_new == NEG_INF ? 0.0f : m_new;
-        if (__builtin_amdgcn_ballot_w64(m_new > m)) {
-            const float alpha = exp2_fast(m - m_use);
+        if (__builtin_amdgcn_ballot_w64(mx > m + RISE)) {
+            const float m_new = fmaxf(m, mx), alpha = m_new == NEG_INF ? 1.0f : exp2_fast(m - m_new);
             l *= alpha;
 #pragma unroll
             for (int d = 0; d < DT; ++d)
@@ -172,25 +207,24 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
                 for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
             m = m_new;
         }
+        const float m_use = m == NEG_INF ? 0.0f : m;             // of a row that has seen nothing yet
         uint32_t p[KT][8];
 #pragma unroll
         for (int k = 0; k < KT; ++k)
 #pragma unroll
             for (int r = 0; r < 16; r += 2) {
-                const float p0 = exp2_fast(fmaf(s[k][r], a.scale_log2, -m_use)), p1 = exp2_fast(fmaf(s[k][r + 1], a.scale_log2, -m_use));
-                l += p0 + p1;
-                p[k][r / 2] = pack_bf16(p0, p1);
+                p[k][r / 2] = pack_bf16(exp2_fast(fmaf(s[k][r], a.scale_log2, -m_use)), exp2_fast(fmaf(s[k][r + 1], a.scale_log2, -m_use)));
+                l = add_pair(p[k][r / 2], l);
             }
         auto v_operand = [&](int t16, int d) {
-            const uint32_t at = v_addr + buffer * TILE + t16 * 16 * ROW;
             union {
                 v4s part[2];
                 u32x4 whole;
             } vf;
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-                vf.part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)(
-                    at + e * 8 * ROW + ((v_piece ^ (4 * d) ^ (2 * e)) << 4)));
+                vf.part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)(v_addr[d][e] +
+                                                                                                          2 * buffer * TILE + t16 * 16 * ROW));
             return vf.whole;
         };
         if (careful.value && masked) {
@@ -232,7 +266,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
                     for (int r = 0; r < 16; ++r)
                         if (count[r] > 0.0f) o[d][r] += sign ? NEG_INF : -NEG_INF;
                 }
-            continue;
+            return;
         }
 #pragma unroll
         for (int t16 = 0; t16 < BN / 16; ++t16) {
@@ -241,6 +275,10 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d] = mfma_32x32x16_bf16(__builtin_bit_cast(v8bf, v_operand(t16, d)), pf, o[d]);
         }
+    };
+    for (int kt = 0; kt < n_tiles; kt += 2) {
+        step(kt, std::integral_constant<int, 0>{});
+        if (kt + 1 < n_tiles) step(kt + 1, std::integral_constant<int, 1>{});
     }
     };
     walk(std::false_type{});
@@ -250,15 +288,34 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
 #pragma unroll
         for (int r = 0; r < 16; ++r) none = fmaf(o[d][r], 0.0f, none);
     if (__builtin_expect(__syncthreads_or(none != 0.0f), 0)) walk(std::true_type{});
+    // O^T to rows of bf16 through this wavefront's part of LDS (all are past the barrier above), so that whole rows go to memory
     const float inv = inverse_sum(sum_over_32(l));
-    if (row < len) {
-        const StaticQuantizer quant(a.y_scale ? *a.y_scale : 1.0f);
-        OutT* y = static_cast<OutT*>(a.y) + (int64_t)(seq_start + row) * a.ldy + (int64_t)head * D;
+    uint8_t* slab = lds + wave * 32 * ROW;
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int r = 0; r < 16; r += 4)
-                store_4(y + 32 * d + 8 * (r >> 2) + 4 * half, o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv, quant);
+        for (int r = 0; r < 16; r += 4)
+            *reinterpret_cast<uint2*>(slab + col * ROW + (((4 * d + (r >> 2)) ^ swizzle<D>(col)) << 4) + 8 * half) =
+                make_uint2(pack_bf16(o[d][r] * inv, o[d][r + 1] * inv), pack_bf16(o[d][r + 2] * inv, o[d][r + 3] * inv));
+    wave_lds_fence();
+    constexpr bool BYTES = sizeof(OutT) == 1;
+    constexpr int LANES = BYTES ? PIECES / 2 : PIECES;           // per row, 16 bytes of the output each
+    const int piece = lane % LANES;
+    OutT* y = static_cast<OutT*>(a.y) + (int64_t)(seq_start + q0 + 32 * wave) * a.ldy + (int64_t)head * D + piece * (16 / (int)sizeof(OutT));
+    const StaticQuantizer quant(BYTES ? *a.y_scale : 1.0f);
+#pragma unroll
+    for (int n = 0; n < LANES / 2; ++n) {
+        const int r = n * (64 / LANES) + lane / LANES;
+        const uint8_t* from = slab + r * ROW;
+        uint4 out;
+        if (BYTES) {
+            const uint4 lo = *reinterpret_cast<const uint4*>(from + (((2 * piece) ^ swizzle<D>(r)) << 4));
+            const uint4 hi = *reinterpret_cast<const uint4*>(from + (((2 * piece + 1) ^ swizzle<D>(r)) << 4));
+            out = make_uint4(quant_bf16(lo.x, lo.y, quant), quant_bf16(lo.z, lo.w, quant), quant_bf16(hi.x, hi.y, quant), quant_bf16(hi.z, hi.w, quant));
+        } else {
+            out = *reinterpret_cast<const uint4*>(from + ((piece ^ swizzle<D>(r)) << 4));
+        }
+        if (q0 + 32 * wave + r < len) *reinterpret_cast<uint4*>(y + (int64_t)r * a.ldy) = out;
     }
 }
 
