@@ -568,48 +568,57 @@ def dpq_calibrate(w: torch.Tensor, u_factor: torch.Tensor, w_scale: torch.Tensor
     return codes, scales, zeros
 
 
-def _rows(t: torch.Tensor, what: str, dtype: torch.dtype = torch.bfloat16):
-    """(heads, head_dim, row stride) of rows of heads, a tensor [tokens, heads, D] whose heads lie side by side."""
+def _rows(t: torch.Tensor, what: str):
+    """(tokens, heads, head_dim, row stride) of bf16 rows of heads, a tensor [tokens, heads, D] whose heads lie side by side."""
     n, h, d = t.shape
-    if t.dtype != dtype or t.stride(2) != 1 or (h > 1 and t.stride(1) != d):
-        raise ValueError(f"{what}: {dtype} [tokens, heads, D] with the heads of a token side by side, got {t.dtype} {tuple(t.shape)} {t.stride()}")
-    return h, d, t.stride(0) if n > 1 else h * d
+    s0, s1, s2 = t.stride()
+    if t.dtype is not torch.bfloat16 or s2 != 1 or (s1 != d and h > 1):
+        raise ValueError(f"{what}: bfloat16 [tokens, heads, D] with the heads of a token side by side, got {t.dtype} {tuple(t.shape)} {t.stride()}")
+    return n, h, d, s0 if n > 1 else h * d
 
 
 def _flat_rows(t: torch.Tensor, n: int, width: int, dtype: torch.dtype, what: str) -> int:
     """Row stride of a tensor [n, width]."""
-    if t.dtype != dtype or tuple(t.shape) != (n, width) or t.stride(1) != 1:
+    s0, s1 = t.stride()
+    if t.dtype is not dtype or t.shape != (n, width) or s1 != 1:
         raise ValueError(f"{what}: {dtype} ({n}, {width}) with contiguous rows, got {t.dtype} {tuple(t.shape)} {t.stride()}")
-    return t.stride(0) if n > 1 else width
+    return s0 if n > 1 else width
 
 
 def _cache_args(k_cache: torch.Tensor, v_cache: torch.Tensor, kv_scales: torch.Tensor | None):
     """(element type, n_pages, page_stride, page_size, kv_heads, head_dim) of caches [pages, kv_heads, page_size, head_dim], bf16 or E4M3
     bytes (uint8, with kv_scales)."""
-    n, hk, p, d = k_cache.shape
-    if k_cache.dtype not in (torch.bfloat16, torch.uint8) or v_cache.dtype != k_cache.dtype or v_cache.shape != k_cache.shape:
-        raise ValueError("key and value caches: both bf16 or both uint8 (E4M3 bytes), of one shape [pages, kv_heads, page_size, head_dim]")
-    for c in (k_cache, v_cache):
-        if c.stride(3) != 1 or c.stride(2) != d or (hk > 1 and c.stride(1) != p * d):
-            raise ValueError("a page of a cache is contiguous")
-    if n > 1 and k_cache.stride(0) != v_cache.stride(0):
-        raise ValueError("key and value caches have one page stride")
-    e4m3 = k_cache.dtype == torch.uint8
-    if e4m3:
+    n, hk, p, d = shape = k_cache.shape
+    strides, dtype = k_cache.stride(), k_cache.dtype
+    if v_cache.dtype is not dtype or v_cache.shape != shape or (v_cache.stride() != strides and not (n * hk == 1 and v_cache.is_contiguous())):
+        raise ValueError("key and value caches have one type, shape [pages, kv_heads, page_size, head_dim] and strides")
+    if strides[3] != 1 or strides[2] != d or (strides[1] != p * d and hk > 1):
+        raise ValueError("a page of a cache is contiguous")
+    if dtype is torch.bfloat16:
+        code = CACHE_BF16
+    elif dtype is torch.uint8:
+        code = CACHE_E4M3
         _vector(kv_scales, torch.float32, 2, "kv_scales of an E4M3 cache")
-    return CACHE_E4M3 if e4m3 else CACHE_BF16, n, k_cache.stride(0) if n > 1 else hk * p * d, p, hk, d
+    else:
+        raise ValueError(f"a cache is bfloat16 or uint8 (E4M3 bytes), got {dtype}")
+    return code, n, strides[0] if n > 1 else hk * p * d, p, hk, d
 
 
 def _vector(t: torch.Tensor, dtype: torch.dtype, n: int, what: str) -> None:
-    if t is None or t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+    if t is None or t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{what}: {n} contiguous {dtype} values")
 
 
 def _same_device(*tensors) -> None:
     """All of them on the current device, where the launch goes."""
+    current = None
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != (torch.cuda.current_device() if _current_device is None else _current_device())):
-            raise ValueError(f"a tensor on {t.device} in a call on the current device")
+        if t is not None:
+            at = t.get_device()                                  # -1: not on a GPU
+            if current is None and at >= 0:
+                current = torch.cuda.current_device() if _current_device is None else _current_device()
+            if at != current:
+                raise ValueError(f"a tensor on {t.device} in a call on the current device")
 
 
 def _pointer(t: torch.Tensor | None):
@@ -647,15 +656,15 @@ def attention_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: 
     """w4a8_attention_prompt: q bf16 [T, H, D], k and v [T, HK, D] (views with a row stride are fine), starts int32 [sequences + 1].
     Returns bf16 [T, H * D], or with y_scale the E4M3 bytes (uint8) that the next layer reads.  softmax_scale: 1 / sqrt(D) if None.
     A new output holds zeros in rows of no sequence."""
-    t = q.shape[0]
-    hq, d, ldq = _rows(q, "q")
-    hk, dk, ldk = _rows(k, "k")
-    hv, dv, ldv = _rows(v, "v")
-    if k.shape != v.shape or k.shape[0] != t or dk != d:
+    t, hq, d, ldq = _rows(q, "q")
+    tk, hk, dk, ldk = _rows(k, "k")
+    tv, hv, dv, ldv = _rows(v, "v")
+    if tk != t or tv != t or hv != hk or dk != d or dv != d:
         raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not belong together")
-    if starts.dim() != 1 or starts.numel() < 1:
+    n_seqs = starts.numel() - 1
+    if n_seqs < 0:
         raise ValueError("starts: one int32 more than there are sequences")
-    _vector(starts, torch.int32, starts.numel(), "starts")
+    _vector(starts, torch.int32, n_seqs + 1, "starts")
     dtype = torch.bfloat16 if y_scale is None else torch.uint8
     if out is None:
         out = torch.zeros((t, hq * d), dtype=dtype, device=q.device)
@@ -663,7 +672,7 @@ def attention_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: 
         _vector(y_scale, torch.float32, 1, "y_scale")
     _same_device(q, k, v, starts, out, y_scale)
     ldy = _flat_rows(out, t, hq * d, dtype, "out")
-    _check(lib().w4a8_attention_prompt(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, starts.data_ptr(), starts.numel() - 1, t, hq,
+    _check(lib().w4a8_attention_prompt(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, starts.data_ptr(), n_seqs, t, hq,
                                        hk, d, 1 if causal else 0, d ** -0.5 if softmax_scale is None else softmax_scale, out.data_ptr(), ldy,
                                        _pointer(y_scale), _stream()), "w4a8_attention_prompt")
     return out
@@ -681,12 +690,11 @@ def attention_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     """w4a8_attention_decode: q bf16 [sequences, H, D], caches [pages, HK, page_size, D], tables int32 [sequences, width], lengths int32
     [sequences], prefix_pages int32 with ceil(prefix_length / page_size) entries.  Returns bf16 [sequences, H * D], or with y_scale
     E4M3 bytes (uint8).  workspace: uint8, attention_decode_workspace_bytes() of them; allocated here if None."""
-    n = q.shape[0]
-    hq, d, ldq = _rows(q, "q")
+    n, hq, d, ldq = _rows(q, "q")
     cache_dtype, n_pages, page_stride, page, hk, dk = _cache_args(k_cache, v_cache, kv_scales)
-    if dk != d or tables.dtype != torch.int32 or tables.dim() != 2 or tables.shape[0] != n or (tables.shape[1] > 1 and tables.stride(1) != 1):
+    rows, width = tables.shape
+    if dk != d or rows != n or tables.dtype is not torch.int32 or (width > 1 and tables.stride(1) != 1):
         raise ValueError(f"q {tuple(q.shape)}, cache {tuple(k_cache.shape)} and int32 tables {tuple(tables.shape)} do not belong together")
-    width = tables.shape[1]
     _vector(lengths, torch.int32, n, "lengths")
     if prefix_length:
         _vector(prefix_pages, torch.int32, -(-prefix_length // page), "prefix_pages")
@@ -712,17 +720,20 @@ def attention_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
 
 def cache_copy_pages(cache: torch.Tensor, src: torch.Tensor, dst: torch.Tensor) -> torch.Tensor:
     """w4a8_cache_copy_pages: cache [planes, pages, ...] of any type, pages contiguous; pages src (int32) -> dst in every plane."""
-    planes, pages = cache.shape[:2]
-    if pages < 1 or cache.numel() == 0 or not cache[0, 0].is_contiguous():
-        raise ValueError("cache: [planes, pages, ...] with contiguous pages")
-    size = cache.element_size()
-    _vector(src, torch.int32, src.numel(), "src")
-    _vector(dst, torch.int32, src.numel(), "dst")
+    shape, strides, size = cache.shape, cache.stride(), cache.element_size()
+    page = size                                                  # bytes
+    for n, s in zip(shape[:1:-1], strides[:1:-1]):
+        if n > 1 and s * size != page:
+            raise ValueError("cache: [planes, pages, ...] with contiguous pages")
+        page *= n
+    copies = src.numel()
+    _vector(src, torch.int32, copies, "src")
+    _vector(dst, torch.int32, copies, "dst")
     _same_device(cache, src, dst)
-    page_bytes = cache[0, 0].numel() * size
-    _check(lib().w4a8_cache_copy_pages(cache.data_ptr(), planes, cache.stride(0) * size if planes > 1 else 0, pages,
-                                       cache.stride(1) * size if pages > 1 else page_bytes, page_bytes, src.data_ptr(), dst.data_ptr(),
-                                       src.numel(), _stream()), "w4a8_cache_copy_pages")
+    planes, pages = shape[0], shape[1]
+    _check(lib().w4a8_cache_copy_pages(cache.data_ptr(), planes, strides[0] * size if planes > 1 else 0, pages,
+                                       strides[1] * size if pages > 1 else page, page, src.data_ptr(), dst.data_ptr(), copies, _stream()),
+           "w4a8_cache_copy_pages")
     return cache
 
 
