@@ -1,27 +1,14 @@
 // Attention inside whole prompts: packed sequences, grouped heads, causal or both ways.
 //   o_i = sum_j softmax_j(q_i . k_j * scale) v_j,   j in i's sequence, j <= i if causal
 // One pass over the keys with a running maximum and sum per row: a workgroup owns 32 rows per wavefront of one query head and walks the
-// sequence's keys 64 at a time.  Both products are formed transposed, S^T = K Q^T and O^T = V^T P^T: a lane then holds one row's
-// scores, its maximum is found in registers (and one exchange with the lane 32 away), and the 16 keys whose scores a lane has
-// are, in the same order, those of the second product's operand: P never leaves the registers.  Keys and values come to LDS by
-// copies that pass no registers, one tile ahead; V^T is read from it by transposing reads.
+// sequence's keys 64 at a time (attention_tile.hpp).  Keys and values come to LDS by copies that pass no registers, one tile ahead.
 #include "attention.hpp"
-#include "attention_device.hpp"
+#include "attention_tile.hpp"
 
 namespace w4a8 {
 namespace {
 
 constexpr int XCDS_A = 8;
-constexpr int BN = 64;                                           // keys per tile
-
-// LDS keeps rows of D bf16 in 16-byte pieces, piece p of row r at p ^ swizzle(r): eight rows next to each other have any one piece in
-// eight different bank groups (the rows a read of K touches), and four rows' 64-byte quarters lie in four (a transposing read of V).
-template <int D> __device__ __forceinline__ constexpr int swizzle(int r) {
-    return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
-}
-
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
 // The sequence and, counted from its end, the tile of rows of unit t (0 .. tiles - 1) of the packed batch; false behind the last.
 template <int BM>
 __device__ __forceinline__ bool find_tile(const int32_t* starts, int n_seqs, int64_t T, int t, int& seq_start, int& len, int& tile) {
@@ -56,9 +43,10 @@ __device__ __forceinline__ bool find_tile(const int32_t* starts, int n_seqs, int
 
 template <int D, int WAVES, bool CAUSAL, typename OutT>
 __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptArgs a, int tiles, int by_head) {
-    constexpr int BM = 32 * WAVES, ROW = 2 * D, PIECES = D / 8, TILE = BN * ROW;
+    using Block = RowBlock<D>;
+    constexpr int BM = 32 * WAVES, BN = TILE_KEYS, ROW = Block::ROW, PIECES = Block::PIECES, TILE = Block::TILE, RPC = Block::RPC;
+    constexpr int DT = Block::DT, KT = Block::KT;
     constexpr int COPIES = TILE / 1024 / WAVES;                  // of 64 lanes x 16 bytes, per wavefront for each of K and V
-    constexpr int KS = D / 16, DT = D / 32, KT = BN / 32;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * TILE];   // K 0, V 0, K 1, V 1; first Q, in K 1 and V 1; at last O, in K 0 and V 0
     static_assert(BM * ROW <= 2 * TILE, "Q and O fit two tiles");
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
@@ -87,7 +75,6 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
 
     const uint8_t* kbase = reinterpret_cast<const uint8_t*>(a.k + (int64_t)seq_start * a.ldk + (int64_t)kv_head * D);
     const uint8_t* vbase = reinterpret_cast<const uint8_t*>(a.v + (int64_t)seq_start * a.ldv + (int64_t)kv_head * D);
-    constexpr int RPC = 1024 / ROW;                              // rows per copy
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
     uint32_t k_from[COPIES], v_from[COPIES];                     // where this lane's 16 bytes of its copies come from, within a tile
 #pragma unroll
@@ -118,47 +105,23 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
             }
         }
     };
-    // LDS addresses: K operand of step s: piece 2s + half of row col (+ 32 kt).  V^T operand (step t of 16 keys, channels 32 dt ..): keys
-    // 16t + 4 half + {0..3} and 8 more, 16 channels per 16 lanes
-    uint32_t k_addr[KS], v_addr[DT][2];
-#pragma unroll
-    for (int i = 0; i < KS; ++i) k_addr[i] = lds_base + col * ROW + (uint32_t)(((half ^ swizzle<D>(col)) ^ (2 * i)) << 4);
-    const int j = lane & 15, g1 = (lane >> 4) & 1;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int r = 4 * half + (j >> 2), piece = 2 * g1 + ((j & 3) >> 1);
-            v_addr[d][e] = lds_base + TILE + (r + 8 * e) * ROW + (j & 1) * 8 + (uint32_t)((piece ^ swizzle<D>(r) ^ (4 * d) ^ (2 * e)) << 4);
-        }
-
-    // Q^T, the second operand of S^T = K Q^T, stays in registers; it comes through LDS, since whole rows are what memory gives fast
-    v8bf qf[KS];
+    Block rows(lds_base, lane);
     {
-        const uint8_t* rows = reinterpret_cast<const uint8_t*>(a.q + (int64_t)(seq_start + q0) * a.ldq + (int64_t)head * D);
+        const uint8_t* from = reinterpret_cast<const uint8_t*>(a.q + (int64_t)(seq_start + q0) * a.ldq + (int64_t)head * D);
 #pragma unroll
         for (int q = 0; q < 32 / RPC; ++q) {
             const int r = 32 * wave + q * RPC + lane / PIECES;
-            lds_dma_16(rows, (uint32_t)min(r, len - 1 - q0) * (uint32_t)(a.ldq * 2) + (uint32_t)(((lane % PIECES) ^ swizzle<D>(r)) * 16),
+            lds_dma_16(from, (uint32_t)min(r, len - 1 - q0) * (uint32_t)(a.ldq * 2) + (uint32_t)(((lane % PIECES) ^ swizzle<D>(r)) * 16),
                        lds_base + 2 * TILE + (32 * wave + q * RPC) * ROW);
         }
         lds_dma_wait_all();                                      // a wavefront copies its own rows
-#pragma unroll
-        for (int i = 0; i < KS; ++i)
-            qf[i] = *reinterpret_cast<__attribute__((address_space(3))) const v8bf*>((uintptr_t)(k_addr[i] + 2 * TILE + wave * 32 * ROW));
+        rows.read_q(2 * TILE + wave * 32 * ROW);
     }
 
     // A weight of zero takes a key out of the sums, unless its value is no number.  So a walk that ends with an output that is none is
     // walked again carefully: there, in tiles that hide keys from some rows, values that are no numbers enter only the rows that see them.
-    v16f o[DT];
-    float m, l;                                                  // maximum of the scores so far (scaled, base 2), this lane's part of the sum
     auto walk = [&](auto careful) {
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
-    m = NEG_INF;
-    l = 0.0f;
+    rows.clear();
     copy_tile(0, 0);
     auto step = [&](int kt, auto buffer_c) {
         constexpr int buffer = decltype(buffer_c)::value;
@@ -168,16 +131,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
         const int key0 = kt * BN;
         if (CAUSAL && key0 > q0 + 32 * wave + 31) return;        // (wave-uniform) no row of this wavefront sees the tile
         v16f s[KT];
-#pragma unroll
-        for (int k = 0; k < KT; ++k) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[k][r] = 0.0f;
-#pragma unroll
-            for (int i = 0; i < KS; ++i) {
-                const v8bf kf = *reinterpret_cast<__attribute__((address_space(3))) const v8bf*>((uintptr_t)(k_addr[i] + 2 * buffer * TILE + k * 32 * ROW));
-                s[k] = mfma_32x32x16_bf16(kf, qf[i], s[k]);
-            }
-        }
+        rows.template scores<buffer>(s);
         const bool masked = key0 + BN > len || (CAUSAL && key0 + BN - 1 > q0 + 32 * wave);
         const int seen = CAUSAL ? min(len, row + 1) : len;       // keys below this one
         // a loop of at most one pass: as a branch the compiler turns it into 32 comparisons and selects in every tile
@@ -192,41 +146,8 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
                     if (32 * k + (r & 3) + 8 * (r >> 2) >= edge) s[k][r] = NEG_INF;
             asm volatile("s_mov_b32 %0, 0" : "=s"(hides));
         }
-        float mx = s[0][0];
-#pragma unroll
-        for (int k = 0; k < KT; ++k)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[k][r]);
-        mx = max_over_32(mx) * a.scale_log2;
-        if (__builtin_amdgcn_ballot_w64(mx > m + RISE)) {
-            const float m_new = fmaxf(m, mx), alpha = m_new == NEG_INF ? 1.0f : exp2_fast(m - m_new);
-            l *= alpha;
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
-            m = m_new;
-        }
-        const float m_use = m == NEG_INF ? 0.0f : m;             // of a row that has seen nothing yet
         uint32_t p[KT][8];
-#pragma unroll
-        for (int k = 0; k < KT; ++k)
-#pragma unroll
-            for (int r = 0; r < 16; r += 2) {
-                p[k][r / 2] = pack_bf16(exp2_fast(fmaf(s[k][r], a.scale_log2, -m_use)), exp2_fast(fmaf(s[k][r + 1], a.scale_log2, -m_use)));
-                l = add_pair(p[k][r / 2], l);
-            }
-        auto v_operand = [&](int t16, int d) {
-            union {
-                v4s part[2];
-                u32x4 whole;
-            } vf;
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-                vf.part[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)(v_addr[d][e] +
-                                                                                                          2 * buffer * TILE + t16 * 16 * ROW));
-            return vf.whole;
-        };
+        rows.weights(s, a.scale_log2, p);
         if (careful.value && masked) {
 #pragma unroll
             for (int d = 0; d < DT; ++d)
@@ -240,7 +161,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
                         int open_to = seen;
                         asm volatile("" : "+v"(open_to));        // formed here each time: registers are short, time is not
                         __builtin_amdgcn_sched_barrier(0);
-                        u32x4 v = v_operand(t16, d), found, sees;
+                        u32x4 v = rows.template v_operand<buffer>(t16, d), found, sees;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             uint32_t number = 0, hit = 0, open = 0;
@@ -257,24 +178,16 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
                             found[i] = hit;
                             sees[i] = open;
                         }
-                        const uint32_t* pk = p[t16 / 2] + 4 * (t16 & 1);
-                        if (sign == 0)
-                            o[d] = mfma_32x32x16_bf16(__builtin_bit_cast(v8bf, v), __builtin_bit_cast(v8bf, u32x4{pk[0], pk[1], pk[2], pk[3]}), o[d]);
+                        if (sign == 0) rows.o[d] = mfma_32x32x16_bf16(__builtin_bit_cast(v8bf, v), Block::p_operand(p, t16), rows.o[d]);
                         count = mfma_32x32x16_bf16(__builtin_bit_cast(v8bf, found), __builtin_bit_cast(v8bf, sees), count);
                     }
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        if (count[r] > 0.0f) o[d][r] += sign ? NEG_INF : -NEG_INF;
+                        if (count[r] > 0.0f) rows.o[d][r] += sign ? NEG_INF : -NEG_INF;
                 }
             return;
         }
-#pragma unroll
-        for (int t16 = 0; t16 < BN / 16; ++t16) {
-            const uint32_t* pk = p[t16 / 2] + 4 * (t16 & 1);
-            const v8bf pf = __builtin_bit_cast(v8bf, u32x4{pk[0], pk[1], pk[2], pk[3]});
-#pragma unroll
-            for (int d = 0; d < DT; ++d) o[d] = mfma_32x32x16_bf16(__builtin_bit_cast(v8bf, v_operand(t16, d)), pf, o[d]);
-        }
+        rows.template add_values<buffer>(p);
     };
     for (int kt = 0; kt < n_tiles; kt += 2) {
         step(kt, std::integral_constant<int, 0>{});
@@ -286,17 +199,17 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) none = fmaf(o[d][r], 0.0f, none);
+        for (int r = 0; r < 16; ++r) none = fmaf(rows.o[d][r], 0.0f, none);
     if (__builtin_expect(__syncthreads_or(none != 0.0f), 0)) walk(std::true_type{});
     // O^T to rows of bf16 through this wavefront's part of LDS (all are past the barrier above), so that whole rows go to memory
-    const float inv = inverse_sum(sum_over_32(l));
+    const float inv = inverse_sum(sum_over_32(rows.l));
     uint8_t* slab = lds + wave * 32 * ROW;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int r = 0; r < 16; r += 4)
             *reinterpret_cast<uint2*>(slab + col * ROW + (((4 * d + (r >> 2)) ^ swizzle<D>(col)) << 4) + 8 * half) =
-                make_uint2(pack_bf16(o[d][r] * inv, o[d][r + 1] * inv), pack_bf16(o[d][r + 2] * inv, o[d][r + 3] * inv));
+                make_uint2(pack_bf16(rows.o[d][r] * inv, rows.o[d][r + 1] * inv), pack_bf16(rows.o[d][r + 2] * inv, rows.o[d][r + 3] * inv));
     wave_lds_fence();
     constexpr bool BYTES = sizeof(OutT) == 1;
     constexpr int LANES = BYTES ? PIECES / 2 : PIECES;           // per row, 16 bytes of the output each
