@@ -8,11 +8,13 @@ using namespace w4a8;
 
 namespace w4a8 {
 
-// A workgroup of the decode kernel reads one range of keys for up to 16 rows.  Ranges of fewer than MIN_RANGE keys would not amortize a
-// workgroup's start and its partial result; enough ranges to give every compute unit some workgroups are what few sequences need.
-DecodePlan decode_plan(int64_t n_seqs, int q_heads, int kv_heads, int64_t own_capacity, int64_t prefix_len) {
-    constexpr int64_t WANTED = 1024, MIN_RANGE = 256, MOST = 64;
-    const int64_t group = q_heads / kv_heads;
+// A workgroup on the sequences' own tokens reads one range of keys for up to 16 rows.  Ranges of fewer than MIN_RANGE keys would not
+// amortize a workgroup's start and its partial result; enough ranges to give every compute unit some workgroups are what few sequences need.
+// On the prefix up to 16 rows go the same way.  More rows walk tiles of 64 keys that 64 or 128 rows share; there a range costs its tiles,
+// about 1 us each with all compute units busy, and every part of a row 4 (D + 2) bytes written and read again, about 4.5 TB/s.
+DecodePlan decode_plan(int64_t n_seqs, int q_heads, int kv_heads, int head_dim, int64_t own_capacity, int64_t prefix_len) {
+    constexpr int64_t WANTED = 1024, MIN_RANGE = 256, MOST = 64, CUS = 256;
+    const int64_t group = q_heads / kv_heads, rows = n_seqs * group;
     auto splits = [&](int64_t units, int64_t keys) {
         int64_t s = (WANTED + units - 1) / units;
         const int64_t most = (keys + MIN_RANGE - 1) / MIN_RANGE;
@@ -21,7 +23,20 @@ DecodePlan decode_plan(int64_t n_seqs, int q_heads, int kv_heads, int64_t own_ca
     };
     DecodePlan p;
     p.own_splits = splits(n_seqs * kv_heads * ((group + 15) / 16), own_capacity);
-    p.prefix_splits = prefix_len > 0 ? splits(kv_heads * ((n_seqs * group + 15) / 16), prefix_len) : 0;
+    p.prefix_splits = 0;
+    p.prefix_rows = rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
+    if (prefix_len > 0 && p.prefix_rows == 16) {
+        p.prefix_splits = splits(kv_heads, prefix_len);
+    } else if (prefix_len > 0) {
+        const int64_t units = kv_heads * ((rows + p.prefix_rows - 1) / p.prefix_rows), tiles = (prefix_len + 63) / 64;
+        const double part_us = (double)n_seqs * q_heads * 8 * (head_dim + 2) / 4.5e6;
+        double best = 0;
+        for (int64_t s = 1; s <= MOST && s <= tiles; ++s) {
+            const int64_t rounds = (units * s + CUS - 1) / CUS;
+            const double us = (double)rounds * ((double)((tiles + s - 1) / s) * p.prefix_rows / 128 + 4) + (double)s * part_us;
+            if (s == 1 || us < best) best = us, p.prefix_splits = (int)s;
+        }
+    }
     p.parts = p.own_splits == 1 && p.prefix_splits == 0 ? 0 : p.own_splits + p.prefix_splits;
     return p;
 }
@@ -164,7 +179,7 @@ static int check_decode(int64_t n_seqs, int32_t q_heads, int32_t kv_heads, int32
 size_t w4a8_attention_decode_workspace_bytes(int64_t n_seqs, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t page_size,
                                              int64_t table_width, int64_t prefix_length) {
     if (check_decode(n_seqs, q_heads, kv_heads, head_dim, page_size, table_width, prefix_length) != W4A8_OK || n_seqs == 0) return 0;
-    return decode_partial_bytes(decode_plan(n_seqs, q_heads, kv_heads, table_width * page_size, prefix_length), n_seqs, q_heads, head_dim);
+    return decode_partial_bytes(decode_plan(n_seqs, q_heads, kv_heads, head_dim, table_width * page_size, prefix_length), n_seqs, q_heads, head_dim);
 }
 
 int w4a8_attention_decode(const void* q_dev, int64_t ldq, int64_t n_seqs, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
@@ -187,7 +202,7 @@ int w4a8_attention_decode(const void* q_dev, int64_t ldq, int64_t n_seqs, int32_
     if (!aligned(k_cache_dev, 16) || !aligned(v_cache_dev, 16) || !aligned(kv_scales_dev, 4) || !aligned(tables_dev, 4) || !aligned(lengths_dev, 4) ||
         !aligned(prefix_pages_dev, 4) || !aligned(y_scale_dev, 4))
         return W4A8_ERR_ALIGN;
-    const DecodePlan p = decode_plan(n_seqs, q_heads, kv_heads, table_width * page_size, prefix_length);
+    const DecodePlan p = decode_plan(n_seqs, q_heads, kv_heads, head_dim, table_width * page_size, prefix_length);
     const size_t need = decode_partial_bytes(p, n_seqs, q_heads, head_dim);
     if (need > 0) {
         if (!workspace_dev) return W4A8_ERR_NULL;

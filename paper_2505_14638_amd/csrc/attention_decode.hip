@@ -7,7 +7,7 @@
 // first operand needs eight keys of a channel in one lane -- a lane loads eight keys by eight channels and turns them in registers.  Memory
 // bounds it: 16 KB of bf16 keys and values per 16 matrix instructions.
 #include "attention.hpp"
-#include "attention_device.hpp"
+#include "attention_tile.hpp"
 
 namespace w4a8 {
 namespace {
@@ -242,6 +242,165 @@ __global__ void __launch_bounds__(64 * WAVES_D, 2) attention_decode_kernel(Decod
     }
 }
 
+// A lane's 16 bytes of `base` + its own offset to LDS byte address lds_addr + 16 * lane, as lds_dma_16, offsets beyond 32 bits.
+__device__ __forceinline__ void lds_dma_16_far(const uint8_t* from, uint32_t lds_addr) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(lds_addr) : "memory", "m0");
+}
+
+// The prefix for many rows: all sequences' rows of a key head, 32 per wavefront, walk a range of the prefix's tokens in tiles of 64 keys,
+// which the wavefronts share in LDS.  Pages are read 16 tokens at a time (sixteen never straddle a page), one tile ahead; E4M3 becomes
+// bf16 on its way to LDS.  Ends in a partial result per row.
+template <int D, bool E4M3, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, WAVES / 2) attention_prefix_kernel(DecodeArgs a, DecodePlan plan, int row_tiles, int units) {
+    using Block = RowBlock<D>;
+    constexpr int BM = 32 * WAVES, ROW = Block::ROW, PIECES = Block::PIECES, TILE = Block::TILE, RPC = Block::RPC, KT = Block::KT;
+    constexpr int GROUPS = 4 / WAVES;                            // of 16 keys, that a wavefront brings of every tile
+    constexpr int SIZE = E4M3 ? 1 : 2, LOADS = 16 * D * SIZE / 1024;   // 64 x 16 bytes per group
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * TILE];
+    static_assert(BM * ROW <= 2 * TILE, "Q fits two tiles");
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+
+    // row tiles of one range of keys run on one XCD, whose L2 then serves the range to all but the first
+    const int per_xcd = (units + 7) / 8;
+    int unit = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8);
+    if ((int)(blockIdx.x / 8) >= per_xcd || unit >= units) return;
+    const int row_tile = unit % row_tiles;
+    unit /= row_tiles;
+    const int split = unit % plan.prefix_splits, kv_head = unit / plan.prefix_splits;
+    const int group = a.q_heads / a.c.kv_heads, n_rows = a.n_seqs * group;
+    const int first = row_tile * BM + 32 * wave;                 // this wavefront's rows: (sequence, query head of the key head)
+    const int tiles = (int)((a.prefix_len + TILE_KEYS - 1) / TILE_KEYS), per = (tiles + plan.prefix_splits - 1) / plan.prefix_splits;
+    const int t_begin = min(split * per, tiles), t_end = min(t_begin + per, tiles);
+
+    Block rows(lds_base, lane);
+    rows.clear();
+    {
+#pragma unroll
+        for (int q = 0; q < 32 / RPC; ++q) {
+            const int r = q * RPC + lane / PIECES, at = min(first + r, n_rows - 1);
+            lds_dma_16_far(reinterpret_cast<const uint8_t*>(a.q + (int64_t)(at / group) * a.ldq + (int64_t)(kv_head * group + at % group) * D) +
+                               ((lane % PIECES) ^ swizzle<D>(r)) * 16,
+                           lds_base + 2 * TILE + (32 * wave + q * RPC) * ROW);
+        }
+        lds_dma_wait_all();
+        rows.read_q(2 * TILE + wave * 32 * ROW);
+    }
+    const float score_scale = a.scale_log2 * (E4M3 ? a.kv_scales[0] : 1.0f);
+
+    // pages of the tile's four groups of 16 keys, in lanes 0..3; -1: no tokens there
+    auto pages_of = [&](int t) {
+        const int64_t key = (int64_t)t * TILE_KEYS + 16 * (lane & 3);
+        const int p = t < t_end && key < a.prefix_len ? a.prefix_pages[key >> a.c.page_shift] : -1;
+        return p < a.c.n_pages ? p : -1;
+    };
+    u32x4 held[E4M3 ? 2 * GROUPS * LOADS : 1];                   // E4M3 on its way to LDS
+    // Brings this wavefront's groups of tile t to the buffer (E4M3: to registers).  Rows behind the prefix's end repeat its last one;
+    // a group without tokens becomes zeros: what no row sees must still be numbers.
+    auto fetch = [&](int t, int pages, int buffer) {
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+            const int grp = wave * GROUPS + g;
+            const int64_t key = (int64_t)t * TILE_KEYS + 16 * grp;
+            const int page = __builtin_amdgcn_readlane(pages, grp);
+            const uint32_t to = lds_base + 2 * buffer * TILE + 16 * grp * ROW;
+            if (page < 0) {
+                if (E4M3) {
+#pragma unroll
+                    for (int i = 0; i < 2 * LOADS; ++i) held[2 * LOADS * g + i] = u32x4{0, 0, 0, 0};
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 2 * LOADS; ++i)
+                        *reinterpret_cast<__attribute__((address_space(3))) u32x4*>((uintptr_t)(to + i / LOADS * TILE + i % LOADS * 1024 + lane * 16)) =
+                            u32x4{0, 0, 0, 0};
+                }
+                continue;
+            }
+            const int64_t at = (page * a.c.page_stride + ((int64_t)kv_head * a.c.page_size + (key & (a.c.page_size - 1))) * D) * SIZE;
+            const int last = (int)(a.prefix_len - 1 - key);      // of the group's rows, if below 15
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                if (E4M3) {
+                    const int byte = (i * 64 + lane) * 16, r = min(byte / D, last);
+                    held[2 * LOADS * g + i] = *reinterpret_cast<const u32x4*>(a.k_cache + at + r * D + byte % D);
+                    held[2 * LOADS * g + LOADS + i] = *reinterpret_cast<const u32x4*>(a.v_cache + at + r * D + byte % D);
+                } else {
+                    const int r = i * RPC + lane / PIECES;
+                    const uint32_t off = (uint32_t)(min(r, last) * ROW + ((lane % PIECES) ^ swizzle<D>(r)) * 16);
+                    lds_dma_16(a.k_cache + at, off, to + i * 1024);
+                    lds_dma_16(a.v_cache + at, off, to + TILE + i * 1024);
+                }
+            }
+        }
+    };
+    auto put = [&](int buffer) {                                 // held E4M3 to LDS as bf16
+#pragma unroll
+        for (int i = 0; i < 2 * GROUPS * LOADS; ++i) {
+            const int g = i / (2 * LOADS), is_v = i / LOADS & 1, byte = (i % LOADS * 64 + lane) * 16, r = byte / D, piece = byte % D / 8;
+            const uint32_t to = lds_base + (2 * buffer + is_v) * TILE + (16 * (wave * GROUPS + g) + r) * ROW;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t w0 = held[i][2 * h], w1 = held[i][2 * h + 1];
+                *reinterpret_cast<__attribute__((address_space(3))) u32x4*>((uintptr_t)(to + (((piece + h) ^ swizzle<D>(r)) << 4))) =
+                    u32x4{e4m3_to_bf16<false>(w0), e4m3_to_bf16<true>(w0), e4m3_to_bf16<false>(w1), e4m3_to_bf16<true>(w1)};
+            }
+        }
+    };
+    int pages = pages_of(t_begin), next_pages = pages_of(t_begin + 1);
+    if (t_begin < t_end) {
+        fetch(t_begin, pages, 0);
+        if (E4M3) put(0);
+    }
+    const bool works = first < n_rows;                           // (wave-uniform) this wavefront has rows
+    auto step = [&](int t, auto buffer_c) {
+        constexpr int buffer = decltype(buffer_c)::value;
+        lds_dma_wait_all();
+        __syncthreads();
+        const uint64_t bad = __builtin_amdgcn_ballot_w64(pages < 0) & 15;
+        pages = next_pages;
+        if (t + 1 < t_end) fetch(t + 1, pages, buffer ^ 1);
+        next_pages = pages_of(t + 2);
+        if (works) {
+            v16f s[KT];
+            rows.template scores<buffer>(s);
+            const int64_t left = a.prefix_len - (int64_t)t * TILE_KEYS;
+            int hides = uniform(left < TILE_KEYS || bad);
+            while (hides) {                                      // a loop of at most one pass, as in the kernel of prompts
+                int edge = (int)min(left, (int64_t)TILE_KEYS) - 4 * half;
+                asm volatile("" : "+v"(edge));
+#pragma unroll
+                for (int k = 0; k < KT; ++k)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (32 * k + (r & 3) + 8 * (r >> 2) >= edge || (bad >> (2 * k + r / 8) & 1)) s[k][r] = NEG_INF;
+                asm volatile("s_mov_b32 %0, 0" : "=s"(hides));
+            }
+            uint32_t p[KT][8];
+            rows.weights(s, score_scale, p);
+            rows.template add_values<buffer>(p);
+        }
+        if (E4M3 && t + 1 < t_end) put(buffer ^ 1);
+    };
+    for (int t = t_begin; t < t_end; t += 2) {
+        step(t, std::integral_constant<int, 0>{});
+        if (t + 1 < t_end) step(t + 1, std::integral_constant<int, 1>{});
+    }
+    const float sum = sum_over_32(rows.l), v_scale = E4M3 ? a.kv_scales[1] : 1.0f;
+    const int r = first + col;
+    if (r >= n_rows) return;
+    const int64_t total = (int64_t)a.n_seqs * a.q_heads, part = plan.own_splits + split;
+    const int64_t at = (int64_t)(r / group) * a.q_heads + kv_head * group + r % group;
+    float* out = a.partial + (part * total + at) * D + 4 * half;
+#pragma unroll
+    for (int d = 0; d < Block::DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<float4*>(out + 32 * d + 2 * i) =
+                make_float4(rows.o[d][i] * v_scale, rows.o[d][i + 1] * v_scale, rows.o[d][i + 2] * v_scale, rows.o[d][i + 3] * v_scale);
+    if (half == 0) reinterpret_cast<float2*>(a.partial + plan.parts * total * D)[part * total + at] = make_float2(rows.m, sum);
+}
+
 // Joins the parts of every row: 16 lanes per row.
 template <int D, typename OutT>
 __global__ void __launch_bounds__(256) attention_join_kernel(DecodeArgs a, int parts) {
@@ -273,10 +432,16 @@ __global__ void __launch_bounds__(256) attention_join_kernel(DecodeArgs a, int p
 template <int D, bool E4M3, typename OutT>
 void launch_typed(const DecodeArgs& a, const DecodePlan& p, hipStream_t st) {
     const int group = a.q_heads / a.c.kv_heads, row_tiles = (group + 15) / 16;
-    const int prefix_row_tiles = (int)(((int64_t)a.n_seqs * group + 15) / 16);
+    const int prefix_row_tiles = (int)(((int64_t)a.n_seqs * group + p.prefix_rows - 1) / p.prefix_rows);
     const int own = a.n_seqs * a.c.kv_heads * row_tiles * p.own_splits, shared = a.c.kv_heads * prefix_row_tiles * p.prefix_splits;
-    hipLaunchKernelGGL((attention_decode_kernel<D, E4M3, OutT>), dim3((unsigned)(own + shared)), dim3(64 * WAVES_D), 0, st, a, p, own,
-                       row_tiles, prefix_row_tiles);
+    const bool apart = shared > 0 && p.prefix_rows > 16;
+    hipLaunchKernelGGL((attention_decode_kernel<D, E4M3, OutT>), dim3((unsigned)(apart ? own : own + shared)), dim3(64 * WAVES_D), 0, st, a, p,
+                       own, row_tiles, prefix_row_tiles);
+    if (apart) {
+        const dim3 grid((unsigned)((shared + 7) / 8 * 8));
+        if (p.prefix_rows == 64) hipLaunchKernelGGL((attention_prefix_kernel<D, E4M3, 2>), grid, dim3(128), 0, st, a, p, prefix_row_tiles, shared);
+        else hipLaunchKernelGGL((attention_prefix_kernel<D, E4M3, 4>), grid, dim3(256), 0, st, a, p, prefix_row_tiles, shared);
+    }
     if (p.parts > 0) {
         const int64_t rows = (int64_t)a.n_seqs * a.q_heads;
         hipLaunchKernelGGL((attention_join_kernel<D, OutT>), dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, st, a, p.parts);

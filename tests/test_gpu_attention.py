@@ -138,7 +138,8 @@ def paged(seed, lengths, prefix, hk, d, page, cache, spare=3, fill=None):
 @pytest.mark.parametrize("lengths,prefix,hq,hk,d,page", [
     ([1], 0, 4, 1, 128, 16), ([1000], 0, 32, 8, 128, 16), ([0, 5, 64, 33], 0, 8, 2, 64, 32), ([300, 1, 0], 40, 6, 2, 128, 16),
     ([0], 1, 2, 2, 64, 16), ([0, 0], 513, 8, 8, 128, 128), ([90] * 5, 777, 40, 2, 128, 64), ([16, 17, 15], 0, 33, 1, 64, 16),
-    ([2000, 31], 95, 24, 8, 64, 128), ([7] * 40, 300, 8, 2, 128, 16),
+    ([2000, 31], 95, 24, 8, 64, 128), ([7] * 40, 300, 8, 2, 128, 16), ([20, 0, 3] * 3, 130, 8, 2, 128, 32), ([5] * 17, 1000, 4, 2, 64, 16),
+    ([1] * 70, 2049, 6, 2, 64, 64),
 ])
 def test_decode(gpu_lib, lengths, prefix, hq, hk, d, page, cache):
     n = len(lengths)
@@ -168,6 +169,23 @@ def test_decode_lengths_and_pages_out_of_range(gpu_lib):
     y = B.attention_decode(q, k, v, ints(tables), ints(told))
     out, size = R.decode(q, R.cache_values(k), R.cache_values(v), tables, told, d)
     assert R.worst(y, out, size) <= 1.0 and (y[2] == 0).all() and (y[3] == 0).all()
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("n,d", [(3, 128), (10, 64), (10, 128), (40, 64), (40, 128)])
+def test_prefix_pages_out_of_range(gpu_lib, n, d, cache):
+    """In each kernel that reads a prefix: by 16 rows, by 64 and by 128."""
+    hq, hk, page, prefix = 8, 2, 16, 500
+    k, v, scales, tables, prefix_pages = paged(9, [3] * n, prefix, hk, d, page, cache, fill=NAN if cache == "bf16" else None)
+    for i, bad in ((0, -1), (5, 1 << 30), (6, k.shape[0]), (7, -1), (8, -9), (31, -1)):
+        prefix_pages[i] = bad
+    q = randn(6, n, hq, d).bfloat16()
+    y = B.attention_decode(q, k, v, ints(tables), ints([3] * n), ints(prefix_pages), prefix, scales)
+    k_scale, v_scale = (None, None) if scales is None else scales.tolist()
+    out, size = R.decode(q, R.cache_values(k, k_scale), R.cache_values(v, v_scale), tables, [3] * n, d, prefix_pages, prefix)
+    assert R.worst(y, out, size) <= 1.0
+    y = B.attention_decode(q, k, v, ints(tables), ints([0] * n), ints([-1] * len(prefix_pages)), prefix, scales)
+    assert (y == 0).all()
 
 
 def test_decode_strides(gpu_lib):
