@@ -10,30 +10,32 @@ namespace w4a8 {
 
 // A workgroup on the sequences' own tokens reads one range of keys for up to 16 rows.  Ranges of fewer than MIN_RANGE keys would not
 // amortize a workgroup's start and its partial result; enough ranges to give every compute unit some workgroups are what few sequences need.
-// On the prefix up to 16 rows go the same way.  More rows walk tiles of 64 keys that 64 or 128 rows share; there a range costs its tiles,
-// about 1 us each with all compute units busy, and every part of a row 4 (D + 2) bytes written and read again, about 4.5 TB/s.
+// Up to ONE_GO tokens one workgroup of eight wavefronts takes them all, however few there are of those: that saves the second launch.
+// On the prefix up to 16 rows go the same way.  More rows walk tiles of 64 keys that 128 rows share; there a range costs its tiles, and
+// every part of a row 4 (D + 2) bytes written and read again, about 4.5 TB/s.
 DecodePlan decode_plan(int64_t n_seqs, int q_heads, int kv_heads, int head_dim, int64_t own_capacity, int64_t prefix_len) {
-    constexpr int64_t WANTED = 1024, MIN_RANGE = 256, MOST = 64, CUS = 256;
-    const int64_t group = q_heads / kv_heads, rows = n_seqs * group;
+    constexpr int64_t WANTED = 512, MIN_RANGE = 128, MOST = 64, CUS = 256, ONE_GO = 512;
+    const int64_t group = q_heads / kv_heads, rows = n_seqs * group, own_units = n_seqs * kv_heads * ((group + 15) / 16);
     auto splits = [&](int64_t units, int64_t keys) {
         int64_t s = (WANTED + units - 1) / units;
         const int64_t most = (keys + MIN_RANGE - 1) / MIN_RANGE;
         s = s < most ? s : most;
         return (int)(s < 1 ? 1 : s > MOST ? MOST : s);
     };
-    DecodePlan p;
-    p.own_splits = splits(n_seqs * kv_heads * ((group + 15) / 16), own_capacity);
-    p.prefix_splits = 0;
-    p.prefix_rows = rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
-    if (prefix_len > 0 && p.prefix_rows == 16) {
+    DecodePlan p{};
+    p.own_waves = 4;
+    p.own_splits = splits(own_units, own_capacity);
+    p.prefix_rows = rows <= 16 ? 16 : 128;
+    if (prefix_len == 0) {
+        if (own_capacity <= ONE_GO && own_units <= CUS) p.own_splits = 1, p.own_waves = 8;
+    } else if (p.prefix_rows == 16) {
         p.prefix_splits = splits(kv_heads, prefix_len);
-    } else if (prefix_len > 0) {
+    } else {
         const int64_t units = kv_heads * ((rows + p.prefix_rows - 1) / p.prefix_rows), tiles = (prefix_len + 63) / 64;
         const double part_us = (double)n_seqs * q_heads * 8 * (head_dim + 2) / 4.5e6;
         double best = 0;
         for (int64_t s = 1; s <= MOST && s <= tiles; ++s) {
-            const int64_t rounds = (units * s + CUS - 1) / CUS;
-            const double us = (double)rounds * ((double)((tiles + s - 1) / s) * p.prefix_rows / 128 + 4) + (double)s * part_us;
+            const double us = (double)((units * s + CUS - 1) / CUS) * (1.6 * (double)((tiles + s - 1) / s) + 4) + (double)s * part_us;
             if (s == 1 || us < best) best = us, p.prefix_splits = (int)s;
         }
     }

@@ -61,7 +61,8 @@ struct DecodeArgs {
 // How a decode call is cut up; a function of sizes alone, so that the workspace can be sized before the call.
 struct DecodePlan {
     int own_splits, prefix_splits;                               // ranges of keys per sequence, of the prefix (0: no prefix)
-    int prefix_rows;                                             // rows of a workgroup on the prefix: 16 (the kernel of the own tokens), 64 or 128
+    int own_waves;                                               // wavefronts of a workgroup on the own tokens: 4, or 8 where it finishes its rows
+    int prefix_rows;                                             // rows of a workgroup on the prefix: 16 (as on the own tokens) or 128
     int parts;                                                   // partial results per row; 0: rows are finished at once
 };
 DecodePlan decode_plan(int64_t n_seqs, int q_heads, int kv_heads, int head_dim, int64_t own_capacity, int64_t prefix_len);

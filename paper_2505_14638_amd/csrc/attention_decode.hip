@@ -12,7 +12,7 @@
 namespace w4a8 {
 namespace {
 
-constexpr int STEP = 32, WAVES_D = 4;
+constexpr int STEP = 32, WAVES_D = 4;                           // keys of a step; wavefronts of most workgroups
 
 // N bytes of a lane's part of a row.
 template <int N> struct Piece;
@@ -33,35 +33,40 @@ template <int D, bool E4M3> __device__ __forceinline__ constexpr int channel(int
     return E4M3 ? 64 * (s / 2) + 16 * kg + 8 * (s & 1) : 32 * s + 8 * kg;
 }
 
-template <int D, bool E4M3, typename OutT>
-__global__ void __launch_bounds__(64 * WAVES_D, 2) attention_decode_kernel(DecodeArgs a, DecodePlan plan, int own_units, int row_tiles,
-                                                                           int prefix_row_tiles) {
+// One workgroup of W wavefronts: up to 16 rows of a key head against a range of one sequence's tokens, or of the prefix's (unit counted
+// from own_units).  OutT: bf16 or E4M3 rows, finished; void: a partial result.
+template <int D, int W> constexpr int stream_lds() { return W * 16 * (D + 4 + 2) * 4; }
+template <int D, bool E4M3, int W, typename OutT>
+__device__ __forceinline__ void stream_keys(const DecodeArgs& a, const DecodePlan& plan, int unit, int own_units, uint8_t* lds) {
     using S = Step<D, E4M3>;
     constexpr int KS = D / 32, VD = D / 16;                      // operands of a key row; channels of a lane's values
-    __shared__ __attribute__((aligned(16))) float lds_o[WAVES_D][16][D];
-    __shared__ float lds_m[WAVES_D][16], lds_l[WAVES_D][16];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int PITCH = D + 4;                                 // floats: rows of the exchange start in different banks
+    float* lds_o = reinterpret_cast<float*>(lds);                // [W][16][PITCH], then maxima and sums [W][16]
+    float *lds_m = lds_o + W * 16 * PITCH, *lds_l = lds_m + W * 16;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int c = lane & 15, kg = lane >> 4;
     const int group = a.q_heads / a.c.kv_heads;
 
     // this workgroup's rows, key head and range of keys
-    const bool prefix = (int)blockIdx.x >= own_units;
-    int unit = prefix ? blockIdx.x - own_units : blockIdx.x;
+    const bool prefix = unit >= own_units;
     int kv_head, part, first_row, rows;
-    int64_t n_keys;
+    int64_t n_keys, listed;                                      // tokens; tokens that the table has room for
     const int32_t* pages;
     if (prefix) {
-        const int rt = unit % prefix_row_tiles;
-        unit /= prefix_row_tiles;
+        const int row_tiles = (a.n_seqs * group + 15) / 16;
+        unit -= own_units;
+        const int rt = unit % row_tiles;
+        unit /= row_tiles;
         const int split = unit % plan.prefix_splits;
         kv_head = unit / plan.prefix_splits;
         part = plan.own_splits + split;
         unit = split;
         first_row = rt * 16;
         rows = a.n_seqs * group;
-        n_keys = a.prefix_len;
+        n_keys = listed = a.prefix_len;
         pages = a.prefix_pages;
     } else {
+        const int row_tiles = (group + 15) / 16;
         part = unit % plan.own_splits;
         unit /= plan.own_splits;
         const int rt = unit % row_tiles;
@@ -71,8 +76,9 @@ __global__ void __launch_bounds__(64 * WAVES_D, 2) attention_decode_kernel(Decod
         unit = part;
         first_row = b * group + rt * 16;
         rows = (b + 1) * group;
-        const int64_t cap = a.table_width << a.c.page_shift, n = a.lengths[b];
-        n_keys = n < 0 ? 0 : n < cap ? n : cap;
+        listed = a.table_width << a.c.page_shift;
+        const int64_t n = a.lengths[b];
+        n_keys = n < 0 ? 0 : n < listed ? n : listed;
         pages = a.tables + b * a.ld_tables;
     }
     // row i of the tile: row first_row + i of (sequence, query head of this key head)
@@ -98,7 +104,7 @@ __global__ void __launch_bounds__(64 * WAVES_D, 2) attention_decode_kernel(Decod
 
     // sixteen keys never straddle a page; a page that is no page holds no tokens
     auto page_at = [&](int64_t key, bool& ok) {
-        const int64_t p = key < k_end ? pages[key >> a.c.page_shift] : -1;
+        const int64_t p = key < listed ? pages[key >> a.c.page_shift] : -1;   // not key < k_end: that waits for the length
         ok = p >= 0 && p < a.c.n_pages;
         return ok ? p : 0;
     };
@@ -143,15 +149,14 @@ __global__ void __launch_bounds__(64 * WAVES_D, 2) attention_decode_kernel(Decod
         }
         float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
         mx = max_over_32(max_over_16(mx)) * score_scale;
-        const float m_new = fmaxf(m, mx);
-        const float m_use = m_new == NEG_INF ? 0.0f : m_new;
-        if (__builtin_amdgcn_ballot_w64(m_new > m)) {
-            const float alpha = exp2_fast(m - m_use);
+        if (__builtin_amdgcn_ballot_w64(mx > m + RISE)) {
+            const float m_new = fmaxf(m, mx), alpha = m_new == NEG_INF ? 1.0f : exp2_fast(m - m_new);
             l *= alpha;
 #pragma unroll
             for (int j = 0; j < VD; ++j) o[j] *= alpha;
             m = m_new;
         }
+        const float m_use = m == NEG_INF ? 0.0f : m;
         float p[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -179,7 +184,7 @@ __global__ void __launch_bounds__(64 * WAVES_D, 2) attention_decode_kernel(Decod
             o[j] = mfma_16x16x32_bf16(__builtin_bit_cast(v8bf, w), pf, o[j]);
         }
     };
-    constexpr int STRIDE = STEP * WAVES_D;
+    constexpr int STRIDE = STEP * W;
     int64_t key = k_begin + STEP * wave;
     S x0, x1;
     bool ok0[2], ok1[2];
@@ -194,31 +199,32 @@ __global__ void __launch_bounds__(64 * WAVES_D, 2) attention_decode_kernel(Decod
         key += STRIDE;
     }
 
-    // the four wavefronts' results joined
+    // the wavefronts' results joined
     l = sum_over_32(sum_over_16(l));
 #pragma unroll
-    for (int j = 0; j < VD; ++j)
+    for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) lds_o[wave][c][VD * (4 * kg + r) + j] = o[j][r];
+        for (int j = 0; j < VD; j += 4)
+            *reinterpret_cast<float4*>(lds_o + (wave * 16 + c) * PITCH + VD * (4 * kg + r) + j) = make_float4(o[j][r], o[j + 1][r], o[j + 2][r], o[j + 3][r]);
     if (kg == 0) {
-        lds_m[wave][c] = m;
-        lds_l[wave][c] = l;
+        lds_m[wave * 16 + c] = m;
+        lds_l[wave * 16 + c] = l;
     }
     __syncthreads();
     const int out_row = threadIdx.x / 16, ch = threadIdx.x % 16 * VD;   // VD channels of a row per thread
-    if (first_row + out_row >= rows) return;
+    if (out_row >= 16 || first_row + out_row >= rows) return;
     float top = NEG_INF, sum = 0.0f, acc[VD];
 #pragma unroll
-    for (int w = 0; w < WAVES_D; ++w) top = fmaxf(top, lds_m[w][out_row]);
+    for (int w = 0; w < W; ++w) top = fmaxf(top, lds_m[w * 16 + out_row]);
 #pragma unroll
     for (int j = 0; j < VD; ++j) acc[j] = 0.0f;
 #pragma unroll
-    for (int w = 0; w < WAVES_D; ++w) {
-        const float mw = lds_m[w][out_row];
+    for (int w = 0; w < W; ++w) {
+        const float mw = lds_m[w * 16 + out_row];
         const float f = mw == NEG_INF ? 0.0f : exp2_fast(mw - top);
-        sum = fmaf(lds_l[w][out_row], f, sum);
+        sum = fmaf(lds_l[w * 16 + out_row], f, sum);
 #pragma unroll
-        for (int j = 0; j < VD; ++j) acc[j] = fmaf(lds_o[w][out_row][ch + j], f, acc[j]);
+        for (int j = 0; j < VD; ++j) acc[j] = fmaf(lds_o[(w * 16 + out_row) * PITCH + ch + j], f, acc[j]);
     }
     if (E4M3) {
         const float vs = a.kv_scales[1];
@@ -227,7 +233,7 @@ __global__ void __launch_bounds__(64 * WAVES_D, 2) attention_decode_kernel(Decod
     }
     const int r = first_row + out_row;
     const int64_t at = (int64_t)(r / group) * a.q_heads + kv_head * group + r % group;   // (sequence, query head)
-    if (plan.parts == 0) {
+    if constexpr (!std::is_void_v<OutT>) {
         const float inv = inverse_sum(sum);
         const StaticQuantizer quant(a.y_scale ? *a.y_scale : 1.0f);
         OutT* y = static_cast<OutT*>(a.y) + (int64_t)(r / group) * a.ldy + (int64_t)(kv_head * group + r % group) * D + ch;
@@ -242,6 +248,12 @@ __global__ void __launch_bounds__(64 * WAVES_D, 2) attention_decode_kernel(Decod
     }
 }
 
+template <int D, bool E4M3, int W, typename OutT>
+__global__ void __launch_bounds__(64 * W, 2) attention_stream_kernel(DecodeArgs a, DecodePlan plan, int own_units) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[stream_lds<D, W>()];
+    stream_keys<D, E4M3, W, OutT>(a, plan, blockIdx.x, own_units, lds);
+}
+
 // A lane's 16 bytes of `base` + its own offset to LDS byte address lds_addr + 16 * lane, as lds_dma_16, offsets beyond 32 bits.
 __device__ __forceinline__ void lds_dma_16_far(const uint8_t* from, uint32_t lds_addr) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(lds_addr) : "memory", "m0");
@@ -250,13 +262,12 @@ __device__ __forceinline__ void lds_dma_16_far(const uint8_t* from, uint32_t lds
 // The prefix for many rows: all sequences' rows of a key head, 32 per wavefront, walk a range of the prefix's tokens in tiles of 64 keys,
 // which the wavefronts share in LDS.  Pages are read 16 tokens at a time (sixteen never straddle a page), one tile ahead; E4M3 becomes
 // bf16 on its way to LDS.  Ends in a partial result per row.
-template <int D, bool E4M3, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, WAVES / 2) attention_prefix_kernel(DecodeArgs a, DecodePlan plan, int row_tiles, int units) {
+template <int D, bool E4M3>
+__device__ __forceinline__ void walk_prefix(const DecodeArgs& a, const DecodePlan& plan, int block, int row_tiles, int units, uint8_t* lds) {
     using Block = RowBlock<D>;
-    constexpr int BM = 32 * WAVES, ROW = Block::ROW, PIECES = Block::PIECES, TILE = Block::TILE, RPC = Block::RPC, KT = Block::KT;
+    constexpr int WAVES = WAVES_D, BM = 32 * WAVES, ROW = Block::ROW, PIECES = Block::PIECES, TILE = Block::TILE, RPC = Block::RPC, KT = Block::KT;
     constexpr int GROUPS = 4 / WAVES;                            // of 16 keys, that a wavefront brings of every tile
     constexpr int SIZE = E4M3 ? 1 : 2, LOADS = 16 * D * SIZE / 1024;   // 64 x 16 bytes per group
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * TILE];
     static_assert(BM * ROW <= 2 * TILE, "Q fits two tiles");
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
@@ -264,8 +275,8 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES / 2) attention_prefix_kernel
 
     // row tiles of one range of keys run on one XCD, whose L2 then serves the range to all but the first
     const int per_xcd = (units + 7) / 8;
-    int unit = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8);
-    if ((int)(blockIdx.x / 8) >= per_xcd || unit >= units) return;
+    int unit = block % 8 * per_xcd + block / 8;
+    if (block / 8 >= per_xcd || unit >= units) return;
     const int row_tile = unit % row_tiles;
     unit /= row_tiles;
     const int split = unit % plan.prefix_splits, kv_head = unit / plan.prefix_splits;
@@ -274,19 +285,6 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES / 2) attention_prefix_kernel
     const int tiles = (int)((a.prefix_len + TILE_KEYS - 1) / TILE_KEYS), per = (tiles + plan.prefix_splits - 1) / plan.prefix_splits;
     const int t_begin = min(split * per, tiles), t_end = min(t_begin + per, tiles);
 
-    Block rows(lds_base, lane);
-    rows.clear();
-    {
-#pragma unroll
-        for (int q = 0; q < 32 / RPC; ++q) {
-            const int r = q * RPC + lane / PIECES, at = min(first + r, n_rows - 1);
-            lds_dma_16_far(reinterpret_cast<const uint8_t*>(a.q + (int64_t)(at / group) * a.ldq + (int64_t)(kv_head * group + at % group) * D) +
-                               ((lane % PIECES) ^ swizzle<D>(r)) * 16,
-                           lds_base + 2 * TILE + (32 * wave + q * RPC) * ROW);
-        }
-        lds_dma_wait_all();
-        rows.read_q(2 * TILE + wave * 32 * ROW);
-    }
     const float score_scale = a.scale_log2 * (E4M3 ? a.kv_scales[0] : 1.0f);
 
     // pages of the tile's four groups of 16 keys, in lanes 0..3; -1: no tokens there
@@ -347,25 +345,41 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES / 2) attention_prefix_kernel
             }
         }
     };
-    int pages = pages_of(t_begin), next_pages = pages_of(t_begin + 1);
-    if (t_begin < t_end) {
-        fetch(t_begin, pages, 0);
-        if (E4M3) put(0);
+    // Fetched a tile before their use, their pages a tile before that.
+    int pages = pages_of(t_begin);
+    uint32_t bad = 0;                                            // four bits a tile, the latest lowest: its groups that hold no tokens
+    auto fetch_next = [&](int t, int buffer) {
+        bad = bad << 4 | ((uint32_t)__builtin_amdgcn_ballot_w64(pages < 0) & 15);
+        const int now = pages;
+        pages = pages_of(t + 1);
+        if (t < t_end) fetch(t, now, buffer);
+    };
+    // the rows of Q, a wavefront's own, on their way together with the first tile
+    Block rows(lds_base, lane);
+    rows.clear();
+#pragma unroll
+    for (int q = 0; q < 32 / RPC; ++q) {
+        const int r = q * RPC + lane / PIECES, at = min(first + r, n_rows - 1);
+        lds_dma_16_far(reinterpret_cast<const uint8_t*>(a.q + (int64_t)(at / group) * a.ldq + (int64_t)(kv_head * group + at % group) * D) +
+                           ((lane % PIECES) ^ swizzle<D>(r)) * 16,
+                       lds_base + 2 * TILE + (32 * wave + q * RPC) * ROW);
     }
+    fetch_next(t_begin, 0);
+    if (E4M3 && t_begin < t_end) put(0);
+    lds_dma_wait_all();
+    rows.read_q(2 * TILE + wave * 32 * ROW);
     const bool works = first < n_rows;                           // (wave-uniform) this wavefront has rows
     auto step = [&](int t, auto buffer_c) {
         constexpr int buffer = decltype(buffer_c)::value;
-        lds_dma_wait_all();
+        if (!E4M3) lds_dma_wait_all();
         __syncthreads();
-        const uint64_t bad = __builtin_amdgcn_ballot_w64(pages < 0) & 15;
-        pages = next_pages;
-        if (t + 1 < t_end) fetch(t + 1, pages, buffer ^ 1);
-        next_pages = pages_of(t + 2);
+        fetch_next(t + 1, buffer ^ 1);
         if (works) {
             v16f s[KT];
             rows.template scores<buffer>(s);
             const int64_t left = a.prefix_len - (int64_t)t * TILE_KEYS;
-            int hides = uniform(left < TILE_KEYS || bad);
+            const uint32_t none = bad >> 4 & 15;                     // of this tile's groups
+            int hides = uniform(left < TILE_KEYS || none);
             while (hides) {                                      // a loop of at most one pass, as in the kernel of prompts
                 int edge = (int)min(left, (int64_t)TILE_KEYS) - 4 * half;
                 asm volatile("" : "+v"(edge));
@@ -373,7 +387,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES / 2) attention_prefix_kernel
                 for (int k = 0; k < KT; ++k)
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        if (32 * k + (r & 3) + 8 * (r >> 2) >= edge || (bad >> (2 * k + r / 8) & 1)) s[k][r] = NEG_INF;
+                        if (32 * k + (r & 3) + 8 * (r >> 2) >= edge || (none >> (2 * k + r / 8) & 1)) s[k][r] = NEG_INF;
                 asm volatile("s_mov_b32 %0, 0" : "=s"(hides));
             }
             uint32_t p[KT][8];
@@ -401,68 +415,127 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES / 2) attention_prefix_kernel
     if (half == 0) reinterpret_cast<float2*>(a.partial + plan.parts * total * D)[part * total + at] = make_float2(rows.m, sum);
 }
 
-// Joins the parts of every row: 16 lanes per row.
+// The prefix for many rows and the sequences' own tokens in one launch: the workgroups on the prefix come first, mostly one for every
+// compute unit or fewer, and those on the own tokens, which memory bounds, run beside them.  256 sequences, 64 heads, 8191 E4M3 tokens in
+// common and 30 .. 1000 of their own: 121 us, where the two take 105 and 62 apart; with twice the workgroups on the prefix, which then leave
+// no room beside them, 156.
+template <int D, bool E4M3>
+__global__ void __launch_bounds__(64 * WAVES_D, 2) attention_shared_kernel(DecodeArgs a, DecodePlan plan, int own_units, int row_tiles, int units,
+                                                                           int prefix_blocks) {
+    constexpr int BYTES = 4 * RowBlock<D>::TILE;
+    static_assert(stream_lds<D, WAVES_D>() <= BYTES, "either body's LDS");
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[BYTES];
+    if ((int)blockIdx.x < prefix_blocks) walk_prefix<D, E4M3>(a, plan, blockIdx.x, row_tiles, units, lds);
+    else stream_keys<D, E4M3, WAVES_D, void>(a, plan, blockIdx.x - prefix_blocks, own_units, lds);
+}
+
+// Joins the parts of a row, a wavefront per row: every lane weighs a part (or two), then sixteen lanes read a part's channels, four parts
+// at a time.
 template <int D, typename OutT>
 __global__ void __launch_bounds__(256) attention_join_kernel(DecodeArgs a, int parts) {
     constexpr int VD = D / 16;
-    const int64_t total = (int64_t)a.n_seqs * a.q_heads, row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
+    const int lane = threadIdx.x & 63;
+    const int64_t total = (int64_t)a.n_seqs * a.q_heads, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= total) return;
-    const int ch = threadIdx.x % 16 * VD;
     const float2* ml = reinterpret_cast<const float2*>(a.partial + parts * total * D) + row;
-    float top = NEG_INF, sum = 0.0f, acc[VD];
+    float2 t[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) t[i] = lane + 64 * i < parts ? ml[(lane + 64 * i) * total] : make_float2(NEG_INF, 0.0f);
+    float top = fmaxf(t[0].x, t[1].x);
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+    top = max_over_32(max_over_16(top));
+    float f[2], sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        f[i] = t[i].x == NEG_INF ? 0.0f : exp2_fast(t[i].x - top);
+        sum = fmaf(t[i].y, f[i], sum);
+    }
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) sum += __shfl_xor(sum, d);
+    sum = sum_over_32(sum_over_16(sum));
+    const int ch = lane % 16 * VD;
+    float acc[VD];
 #pragma unroll
     for (int j = 0; j < VD; ++j) acc[j] = 0.0f;
-    for (int p = 0; p < parts; ++p) top = fmaxf(top, ml[p * total].x);
-    for (int p = 0; p < parts; ++p) {
-        const float2 t = ml[p * total];
-        if (t.x == NEG_INF) continue;
-        const float f = exp2_fast(t.x - top);
-        sum = fmaf(t.y, f, sum);
-        const float* part = a.partial + (p * total + row) * D + ch;
+    const float* from = a.partial + row * D + ch;
+    for (int base = 0; base < parts; base += 16) {
+        float4 x[4][VD / 4];
+        float w[4];
 #pragma unroll
-        for (int j = 0; j < VD; ++j) acc[j] = fmaf(part[j], f, acc[j]);
+        for (int i = 0; i < 4; ++i) {
+            if (base + 4 * i >= parts) {
+                w[i] = 0.0f;
+                continue;
+            }
+            const int p = base + 4 * i + lane / 16;
+            w[i] = __shfl(base < 64 ? f[0] : f[1], p & 63);      // (no part: weight 0)
+            const float* at = from + (p < parts ? p : 0) * total * D;
+#pragma unroll
+            for (int j = 0; j < VD / 4; ++j) x[i][j] = *reinterpret_cast<const float4*>(at + 4 * j);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (w[i] == 0.0f) continue;                          // a part of no keys holds zeros, or nothing at all
+#pragma unroll
+            for (int j = 0; j < VD / 4; ++j) {
+                acc[4 * j] = fmaf(x[i][j].x, w[i], acc[4 * j]);
+                acc[4 * j + 1] = fmaf(x[i][j].y, w[i], acc[4 * j + 1]);
+                acc[4 * j + 2] = fmaf(x[i][j].z, w[i], acc[4 * j + 2]);
+                acc[4 * j + 3] = fmaf(x[i][j].w, w[i], acc[4 * j + 3]);
+            }
+        }
     }
     const float inv = inverse_sum(sum);
+#pragma unroll
+    for (int j = 0; j < VD; ++j) acc[j] = sum_over_32(sum_over_16(acc[j])) * inv;
+    if (lane >= 16) return;
     const StaticQuantizer quant(a.y_scale ? *a.y_scale : 1.0f);
     OutT* y = static_cast<OutT*>(a.y) + row / a.q_heads * a.ldy + row % a.q_heads * D + ch;
 #pragma unroll
-    for (int j = 0; j < VD; j += 4) store_4(y + j, acc[j] * inv, acc[j + 1] * inv, acc[j + 2] * inv, acc[j + 3] * inv, quant);
+    for (int j = 0; j < VD; j += 4) store_4(y + j, acc[j], acc[j + 1], acc[j + 2], acc[j + 3], quant);
 }
 
-template <int D, bool E4M3, typename OutT>
-void launch_typed(const DecodeArgs& a, const DecodePlan& p, hipStream_t st) {
-    const int group = a.q_heads / a.c.kv_heads, row_tiles = (group + 15) / 16;
-    const int prefix_row_tiles = (int)(((int64_t)a.n_seqs * group + p.prefix_rows - 1) / p.prefix_rows);
-    const int own = a.n_seqs * a.c.kv_heads * row_tiles * p.own_splits, shared = a.c.kv_heads * prefix_row_tiles * p.prefix_splits;
-    const bool apart = shared > 0 && p.prefix_rows > 16;
-    hipLaunchKernelGGL((attention_decode_kernel<D, E4M3, OutT>), dim3((unsigned)(apart ? own : own + shared)), dim3(64 * WAVES_D), 0, st, a, p,
-                       own, row_tiles, prefix_row_tiles);
-    if (apart) {
-        const dim3 grid((unsigned)((shared + 7) / 8 * 8));
-        if (p.prefix_rows == 64) hipLaunchKernelGGL((attention_prefix_kernel<D, E4M3, 2>), grid, dim3(128), 0, st, a, p, prefix_row_tiles, shared);
-        else hipLaunchKernelGGL((attention_prefix_kernel<D, E4M3, 4>), grid, dim3(256), 0, st, a, p, prefix_row_tiles, shared);
-    }
-    if (p.parts > 0) {
-        const int64_t rows = (int64_t)a.n_seqs * a.q_heads;
-        hipLaunchKernelGGL((attention_join_kernel<D, OutT>), dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, st, a, p.parts);
-    }
+template <int D, bool E4M3, int W, typename OutT>
+void launch_stream(const DecodeArgs& a, const DecodePlan& p, int own, int shared, hipStream_t st) {
+    hipLaunchKernelGGL((attention_stream_kernel<D, E4M3, W, OutT>), dim3((unsigned)(own + shared)), dim3(64 * W), 0, st, a, p, own);
 }
 
 template <int D, bool E4M3>
-void launch_out(const DecodeArgs& a, const DecodePlan& p, hipStream_t st) {
-    if (a.y_scale) launch_typed<D, E4M3, uint8_t>(a, p, st);
-    else launch_typed<D, E4M3, uint16_t>(a, p, st);
+void launch_typed(const DecodeArgs& a, const DecodePlan& p, hipStream_t st) {
+    const int group = a.q_heads / a.c.kv_heads;
+    const int row_tiles = (int)(((int64_t)a.n_seqs * group + p.prefix_rows - 1) / p.prefix_rows);
+    const int own = a.n_seqs * a.c.kv_heads * ((group + 15) / 16) * p.own_splits, shared = a.c.kv_heads * row_tiles * p.prefix_splits;
+    if (p.parts == 0) {
+        if (p.own_waves == 8) {
+            if (a.y_scale) launch_stream<D, E4M3, 8, uint8_t>(a, p, own, 0, st);
+            else launch_stream<D, E4M3, 8, uint16_t>(a, p, own, 0, st);
+        } else {
+            if (a.y_scale) launch_stream<D, E4M3, WAVES_D, uint8_t>(a, p, own, 0, st);
+            else launch_stream<D, E4M3, WAVES_D, uint16_t>(a, p, own, 0, st);
+        }
+        return;
+    }
+    if (p.prefix_rows == 16 || shared == 0) {
+        launch_stream<D, E4M3, WAVES_D, void>(a, p, own, shared, st);
+    } else {
+        const int blocks = (shared + 7) / 8 * 8;
+        hipLaunchKernelGGL((attention_shared_kernel<D, E4M3>), dim3((unsigned)(blocks + own)), dim3(64 * WAVES_D), 0, st, a, p, own, row_tiles, shared, blocks);
+    }
+    const dim3 grid((unsigned)(((int64_t)a.n_seqs * a.q_heads + 3) / 4));
+    if (a.y_scale) hipLaunchKernelGGL((attention_join_kernel<D, uint8_t>), grid, dim3(256), 0, st, a, p.parts);
+    else hipLaunchKernelGGL((attention_join_kernel<D, uint16_t>), grid, dim3(256), 0, st, a, p.parts);
 }
 
 }  // namespace
 
 int launch_attention_decode(const DecodeArgs& a, const DecodePlan& p, hipStream_t st) {
     if (a.c.head_dim == 128) {
-        if (a.c.e4m3) launch_out<128, true>(a, p, st);
-        else launch_out<128, false>(a, p, st);
+        if (a.c.e4m3) launch_typed<128, true>(a, p, st);
+        else launch_typed<128, false>(a, p, st);
     } else {
-        if (a.c.e4m3) launch_out<64, true>(a, p, st);
-        else launch_out<64, false>(a, p, st);
+        if (a.c.e4m3) launch_typed<64, true>(a, p, st);
+        else launch_typed<64, false>(a, p, st);
     }
     return launch_status();
 }

@@ -114,6 +114,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
             lds_dma_16(from, (uint32_t)min(r, len - 1 - q0) * (uint32_t)(a.ldq * 2) + (uint32_t)(((lane % PIECES) ^ swizzle<D>(r)) * 16),
                        lds_base + 2 * TILE + (32 * wave + q * RPC) * ROW);
         }
+        copy_tile(0, 0);                                         // on its way together with them
         lds_dma_wait_all();                                      // a wavefront copies its own rows
         rows.read_q(2 * TILE + wave * 32 * ROW);
     }
@@ -122,7 +123,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
     // walked again carefully: there, in tiles that hide keys from some rows, values that are no numbers enter only the rows that see them.
     auto walk = [&](auto careful) {
     rows.clear();
-    copy_tile(0, 0);
+    if (careful.value) copy_tile(0, 0);
     auto step = [&](int kt, auto buffer_c) {
         constexpr int buffer = decltype(buffer_c)::value;
         lds_dma_wait_all();
