@@ -4,23 +4,24 @@
 
 #include <math.h>
 
+#include <algorithm>
+
 using namespace w4a8;
 
 namespace w4a8 {
 
-// A workgroup on the sequences' own tokens reads one range of keys for up to 16 rows.  Ranges of fewer than MIN_RANGE keys would not
-// amortize a workgroup's start and its partial result; enough ranges to give every compute unit some workgroups are what few sequences need.
+// A workgroup on the sequences' own tokens reads one range of keys for up to 16 rows.  Few sequences need enough ranges to give every
+// compute unit two workgroups (FILL), of SHORT keys at least; more of them cost more by their starts and partial results than they even out (64
+// sequences of 200 .. 8192 tokens, 64 heads, E4M3: 131 us with one range, 152 with up to eight).
 // Up to ONE_GO tokens one workgroup of eight wavefronts takes them all, however few there are of those: that saves the second launch.
 // On the prefix up to 16 rows go the same way.  More rows walk tiles of 64 keys that 128 rows share; there a range costs its tiles, and
 // every part of a row 4 (D + 2) bytes written and read again, about 4.5 TB/s.
 DecodePlan decode_plan(int64_t n_seqs, int q_heads, int kv_heads, int head_dim, int64_t own_capacity, int64_t prefix_len) {
-    constexpr int64_t WANTED = 512, MIN_RANGE = 128, MOST = 64, CUS = 256, ONE_GO = 512;
+    constexpr int64_t FILL = 512, SHORT = 128, MOST = 64, CUS = 256, ONE_GO = 512;
     const int64_t group = q_heads / kv_heads, rows = n_seqs * group, own_units = n_seqs * kv_heads * ((group + 15) / 16);
     auto splits = [&](int64_t units, int64_t keys) {
-        int64_t s = (WANTED + units - 1) / units;
-        const int64_t most = (keys + MIN_RANGE - 1) / MIN_RANGE;
-        s = s < most ? s : most;
-        return (int)(s < 1 ? 1 : s > MOST ? MOST : s);
+        const int64_t s = std::min((FILL + units - 1) / units, (keys + SHORT - 1) / SHORT);
+        return (int)std::max<int64_t>(1, std::min(s, MOST));
     };
     DecodePlan p{};
     p.own_waves = 4;

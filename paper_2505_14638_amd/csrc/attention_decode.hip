@@ -102,18 +102,23 @@ __device__ __forceinline__ void stream_keys(const DecodeArgs& a, const DecodePla
     for (int j = 0; j < VD; ++j) o[j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     float m = NEG_INF, l = 0.0f;
 
-    // sixteen keys never straddle a page; a page that is no page holds no tokens
-    auto page_at = [&](int64_t key, bool& ok) {
-        const int64_t p = key < listed ? pages[key >> a.c.page_shift] : -1;   // not key < k_end: that waits for the length
-        ok = p >= 0 && p < a.c.n_pages;
-        return ok ? p : 0;
+    // Sixteen keys never straddle a page; a page that is no page holds no tokens.  The page numbers of this wavefront's next 32 steps
+    // are in its lanes (step n's in 2 n and 2 n + 1), so that a step does not wait for them.
+    constexpr int STRIDE = STEP * W;
+    int listing = -1;
+    auto list_pages = [&](int64_t key) {                         // of the steps from `key` on
+        const int64_t mine = key + (int64_t)(lane >> 1) * STRIDE + 16 * (lane & 1);
+        const int p = mine < listed ? pages[mine >> a.c.page_shift] : -1;   // not mine < k_end: that waits for the length
+        listing = p < a.c.n_pages ? p : -1;
     };
-    auto load = [&](S& x, int64_t key, bool (&ok)[2]) {
+    auto load = [&](S& x, int64_t key, int n, bool (&ok)[2]) {   // step n of this wavefront, at `key`
+        if (n > 0 && (n & 31) == 0) list_pages(key);
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
+            const int page = __builtin_amdgcn_readlane(listing, 2 * (n & 31) + kt);
+            ok[kt] = page >= 0;
             const int64_t base = key + 16 * kt;
-            const int64_t page = page_at(base, ok[kt]);
-            const int64_t at = page * a.c.page_stride + ((int64_t)kv_head * a.c.page_size + (base & (a.c.page_size - 1))) * D;
+            const int64_t at = (ok[kt] ? page : 0) * a.c.page_stride + ((int64_t)kv_head * a.c.page_size + (base & (a.c.page_size - 1))) * D;
             const uint8_t* kp = a.k_cache + at * S::SIZE;
             const uint8_t* vp = a.v_cache + at * S::SIZE;
 #pragma unroll
@@ -184,17 +189,17 @@ __device__ __forceinline__ void stream_keys(const DecodeArgs& a, const DecodePla
             o[j] = mfma_16x16x32_bf16(__builtin_bit_cast(v8bf, w), pf, o[j]);
         }
     };
-    constexpr int STRIDE = STEP * W;
-    int64_t key = k_begin + STEP * wave;
     S x0, x1;
     bool ok0[2], ok1[2];
-    if (key < k_end) load(x0, key, ok0);
-    while (key < k_end) {
-        if (key + STRIDE < k_end) load(x1, key + STRIDE, ok1);
+    int64_t key = k_begin + STEP * wave;
+    list_pages(key);
+    if (key < k_end) load(x0, key, 0, ok0);
+    for (int n = 0; key < k_end; n += 2) {
+        if (key + STRIDE < k_end) load(x1, key + STRIDE, n + 1, ok1);
         compute(x0, key, ok0);
         key += STRIDE;
         if (key >= k_end) break;
-        if (key + STRIDE < k_end) load(x0, key + STRIDE, ok0);
+        if (key + STRIDE < k_end) load(x0, key + STRIDE, n + 2, ok0);
         compute(x1, key, ok1);
         key += STRIDE;
     }
@@ -242,6 +247,7 @@ __device__ __forceinline__ void stream_keys(const DecodeArgs& a, const DecodePla
     } else {
         const int64_t total = (int64_t)a.n_seqs * a.q_heads;
         float* out = a.partial + (part * total + at) * D + ch;
+        if (k_begin < k_end)                                     // (what nothing is in is not read either)
 #pragma unroll
         for (int j = 0; j < VD; j += 4) *reinterpret_cast<float4*>(out + j) = make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
         if (ch == 0) reinterpret_cast<float2*>(a.partial + plan.parts * total * D)[part * total + at] = make_float2(top, sum);
@@ -469,14 +475,14 @@ __global__ void __launch_bounds__(256) attention_join_kernel(DecodeArgs a, int p
                 continue;
             }
             const int p = base + 4 * i + lane / 16;
-            w[i] = __shfl(base < 64 ? f[0] : f[1], p & 63);      // (no part: weight 0)
-            const float* at = from + (p < parts ? p : 0) * total * D;
+            w[i] = __shfl(base < 64 ? f[0] : f[1], p & 63);      // (no part, or one that is empty: 0)
+            if (w[i] == 0.0f) continue;
 #pragma unroll
-            for (int j = 0; j < VD / 4; ++j) x[i][j] = *reinterpret_cast<const float4*>(at + 4 * j);
+            for (int j = 0; j < VD / 4; ++j) x[i][j] = *reinterpret_cast<const float4*>(from + p * total * D + 4 * j);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (w[i] == 0.0f) continue;                          // a part of no keys holds zeros, or nothing at all
+            if (w[i] == 0.0f) continue;
 #pragma unroll
             for (int j = 0; j < VD / 4; ++j) {
                 acc[4 * j] = fmaf(x[i][j].x, w[i], acc[4 * j]);
