@@ -9,7 +9,21 @@ namespace w4a8 {
 namespace {
 
 constexpr int XCDS_A = 8;
-// The sequence and, counted from its end, the tile of rows of unit t (0 .. tiles - 1) of the packed batch; false behind the last.
+// Sum over the wavefront.
+__device__ __forceinline__ int wave_sum(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xF, 0xF, true);      // lanes 1, 0, 3, 2
+    x += __builtin_amdgcn_update_dpp(0, x, 0x4E, 0xF, 0xF, true);      // lanes 2, 3, 0, 1
+    x += __builtin_amdgcn_update_dpp(0, x, 0x141, 0xF, 0xF, true);     // mirrored in eight
+    x += __builtin_amdgcn_update_dpp(0, x, 0x140, 0xF, 0xF, true);     // mirrored in sixteen
+    auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = (int)(p[0] + p[1]);
+    p = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return uniform((int)(p[0] + p[1]));
+}
+
+// Unit t (0 .. tiles - 1) of the packed batch: a sequence and a tile of its rows; false behind the last.  Causal tiles cost what their place
+// in the sequence says, so up to 64 sequences (a lane each) give their tiles in falling order of it, all the sequences' together: the
+// long ones start first.  More sequences come one after the other, each from its end.
 template <int BM>
 __device__ __forceinline__ bool find_tile(const int32_t* starts, int n_seqs, int64_t T, int t, int& seq_start, int& len, int& tile) {
     const int lane = threadIdx.x & 63;
@@ -22,21 +36,39 @@ __device__ __forceinline__ bool find_tile(const int32_t* starts, int n_seqs, int
             n = hi > lo ? (int)(hi - lo) : 0;
         }
         const int mine = (n + BM - 1) / BM;
-        int upto = mine;                                         // tiles of this sequence and of those before it
+        int first;                                               // the lane of the sequence
+        if (n_seqs <= 64) {
+            if (t >= wave_sum(mine)) return false;
+            // the place: the lowest that at most t tiles lie behind
+            int low = 0, high = (int)((T + BM - 1) / BM);
+            while (low < high) {
+                const int middle = (low + high) >> 1;
+                if (wave_sum(max(0, mine - 1 - middle)) <= t) high = middle;
+                else low = middle + 1;
+            }
+            const int rank = t - wave_sum(max(0, mine - 1 - low));   // among the sequences that reach there
+            const uint64_t reach = __builtin_amdgcn_ballot_w64(mine > low);
+            const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(reach >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)reach, 0));
+            first = __builtin_ctzll(__builtin_amdgcn_ballot_w64(mine > low && before == rank));
+            tile = low;
+        } else {
+            int upto = mine;                                     // tiles of this sequence and of those before it
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int other = __shfl_up(upto, d);
-            if (lane >= d) upto += other;
-        }
-        const uint64_t here = __builtin_amdgcn_ballot_w64(t < upto);
-        if (here) {
-            const int first = __builtin_ctzll(here);
-            seq_start = __builtin_amdgcn_readlane(b, first);
-            len = __builtin_amdgcn_readlane(n, first);
+            for (int d = 1; d < 64; d <<= 1) {
+                const int other = __shfl_up(upto, d);
+                if (lane >= d) upto += other;
+            }
+            const uint64_t here = __builtin_amdgcn_ballot_w64(t < upto);
+            if (!here) {
+                t -= __builtin_amdgcn_readlane(upto, 63);
+                continue;
+            }
+            first = __builtin_ctzll(here);
             tile = __builtin_amdgcn_readlane(upto, first) - 1 - t;
-            return true;
         }
-        t -= __builtin_amdgcn_readlane(upto, 63);
+        seq_start = __builtin_amdgcn_readlane(b, first);
+        len = __builtin_amdgcn_readlane(n, first);
+        return true;
     }
     return false;
 }
