@@ -73,14 +73,29 @@ __device__ __forceinline__ bool find_tile(const int32_t* starts, int n_seqs, int
     return false;
 }
 
-template <int D, int WAVES, bool CAUSAL, typename OutT>
-__global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptArgs a, int tiles, int by_head) {
-    using Block = RowBlock<D>;
-    constexpr int BM = 32 * WAVES, BN = TILE_KEYS, ROW = Block::ROW, PIECES = Block::PIECES, TILE = Block::TILE, RPC = Block::RPC;
+// What becomes of two bf16 values in a walk: themselves; zero instead of what is no number; or one for +infinity (-infinity) and NaN and zero
+// for all else.
+enum Walk { PLAIN = 0, NUMBERS = 1, PLUS = 2, MINUS = 3 };
+__device__ __forceinline__ uint32_t seen_by(int walk, uint32_t w) {
+    uint32_t r = 0;
+#pragma unroll
+    for (int u = 0; u < 32; u += 16) {
+        const uint32_t x = (w >> u) & 0xFFFFu;
+        const bool none = (x & 0x7F80u) == 0x7F80u, nan = none && (x & 0x7Fu);
+        if (walk == NUMBERS) r |= (none ? 0u : x) << u;
+        else r |= (nan || (none && (int)(x >> 15) == walk - PLUS) ? 0x3F80u : 0u) << u;
+    }
+    return r;
+}
+
+template <int D, int WAVES, int BN, bool CAUSAL, typename OutT>
+__global__ void __launch_bounds__(64 * WAVES, BN == 32 ? 3 : 2) attention_prompt_kernel(PromptArgs a, int tiles, int by_head) {
+    using Block = RowBlock<D, BN>;
+    constexpr int BM = 32 * WAVES, ROW = Block::ROW, PIECES = Block::PIECES, TILE = Block::TILE, RPC = Block::RPC;
     constexpr int DT = Block::DT, KT = Block::KT;
     constexpr int COPIES = TILE / 1024 / WAVES;                  // of 64 lanes x 16 bytes, per wavefront for each of K and V
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * TILE];   // K 0, V 0, K 1, V 1; first Q, in K 1 and V 1; at last O, in K 0 and V 0
-    static_assert(BM * ROW <= 2 * TILE, "Q and O fit two tiles");
+    // K 0, V 0, K 1, V 1; first Q, from K 1 on; at last O, from K 0 on
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * TILE + (2 * TILE > BM * ROW ? 2 * TILE : BM * ROW)];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
     const int group = a.q_heads / a.kv_heads;
@@ -116,24 +131,33 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
         k_from[q] = (uint32_t)r * (uint32_t)(a.ldk * 2) + piece;
         v_from[q] = (uint32_t)r * (uint32_t)(a.ldv * 2) + piece;
     }
+    int walk = PLAIN;
     auto copy_tile = [&](int kt, int buffer) {
         const uint8_t* kt_base = kbase + (int64_t)kt * BN * a.ldk * 2;
         const uint8_t* vt_base = vbase + (int64_t)kt * BN * a.ldv * 2;
         const uint32_t to = lds_base + 2 * buffer * TILE + wave * COPIES * 1024;
-        const int left = len - kt * BN;                          // rows behind the sequence's last one are that one
-        if (left >= BN) {
+        const int left = len - kt * BN;
+        if (left >= BN && walk == PLAIN) {
 #pragma unroll
             for (int q = 0; q < COPIES; ++q) {
                 lds_dma_16(kt_base, k_from[q], to + q * 1024);
                 lds_dma_16(vt_base, v_from[q], to + TILE + q * 1024);
             }
-        } else {
+            return;
+        }
+#pragma unroll 1
+        for (int q = 0; q < COPIES; ++q) {
+            const int r = (wave * COPIES + q) * RPC + lane / PIECES, from = min(r, left - 1);   // behind the sequence's last row: that one again
+            const uint32_t piece = (uint32_t)(((lane % PIECES) ^ swizzle<D>(r)) * 16);
+            const uint32_t v_at = (uint32_t)from * (uint32_t)(a.ldv * 2) + piece, here = (uint32_t)uniform((int)(to + q * 1024));
+            lds_dma_16(kt_base, (uint32_t)from * (uint32_t)(a.ldk * 2) + piece, here);
+            if (walk == PLAIN) {
+                lds_dma_16(vt_base, v_at, here + TILE);
+            } else {
+                u32x4 v = *reinterpret_cast<const u32x4*>(vt_base + v_at);
 #pragma unroll
-            for (int q = 0; q < COPIES; ++q) {
-                const int r = (wave * COPIES + q) * RPC + lane / PIECES;
-                const uint32_t back = r < left ? 0u : (uint32_t)(r - left + 1);
-                lds_dma_16(kt_base, k_from[q] - back * (uint32_t)(a.ldk * 2), to + q * 1024);
-                lds_dma_16(vt_base, v_from[q] - back * (uint32_t)(a.ldv * 2), to + TILE + q * 1024);
+                for (int i = 0; i < 4; ++i) v[i] = seen_by(walk, v[i]);
+                lds_write(here + TILE + lane * 16, v);
             }
         }
     };
@@ -151,11 +175,12 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
         rows.read_q(2 * TILE + wave * 32 * ROW);
     }
 
-    // A weight of zero takes a key out of the sums, unless its value is no number.  So a walk that ends with an output that is none is
-    // walked again carefully: there, in tiles that hide keys from some rows, values that are no numbers enter only the rows that see them.
-    auto walk = [&](auto careful) {
+    // A weight of zero takes a key out of the sums, unless its value is no number.  So if an output is none, the rows are walked again with zeros
+    // for such values, and then twice to mark the outputs that see one: all scores are zero there, and every row counts the ones it sees.
+    uint64_t marked = 0;                                         // outputs of this lane that see +infinity or NaN
+    for (;; ++walk) {
     rows.clear();
-    if (careful.value) copy_tile(0, 0);
+    if (walk != PLAIN) copy_tile(0, 0);
     auto step = [&](int kt, auto buffer_c) {
         constexpr int buffer = decltype(buffer_c)::value;
         lds_dma_wait_all();
@@ -165,6 +190,13 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
         if (CAUSAL && key0 > q0 + 32 * wave + 31) return;        // (wave-uniform) no row of this wavefront sees the tile
         v16f s[KT];
         rows.template scores<buffer>(s);
+        for (int counts = uniform(walk >= PLUS); counts;) {      // (a loop of at most one pass, as below)
+#pragma unroll
+            for (int k = 0; k < KT; ++k)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[k][r] = 0.0f;
+            asm volatile("s_mov_b32 %0, 0" : "=s"(counts));
+        }
         const bool masked = key0 + BN > len || (CAUSAL && key0 + BN - 1 > q0 + 32 * wave);
         const int seen = CAUSAL ? min(len, row + 1) : len;       // keys below this one
         // a loop of at most one pass: as a branch the compiler turns it into 32 comparisons and selects in every tile
@@ -181,108 +213,89 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_prompt_kernel(PromptA
         }
         uint32_t p[KT][8];
         rows.weights(s, a.scale_log2, p);
-        if (careful.value && masked) {
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll 1
-                for (int sign = 0; sign < 2; ++sign) {           // +infinity and NaN, then -infinity and NaN
-                    v16f count;                                  // of such values that the row sees
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) count[r] = 0.0f;
-#pragma unroll
-                    for (int t16 = 0; t16 < BN / 16; ++t16) {
-                        int open_to = seen;
-                        asm volatile("" : "+v"(open_to));        // formed here each time: registers are short, time is not
-                        __builtin_amdgcn_sched_barrier(0);
-                        u32x4 v = rows.template v_operand<buffer>(t16, d), found, sees;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            uint32_t number = 0, hit = 0, open = 0;
-#pragma unroll
-                            for (int u = 0; u < 2; ++u) {
-                                const uint32_t x = (v[i] >> (16 * u)) & 0xFFFFu;
-                                const bool none = (x & 0x7F80u) == 0x7F80u, nan = none && (x & 0x7Fu);
-                                const int e = 2 * i + u;
-                                if (!none) number |= x << (16 * u);
-                                if (nan || (none && (x >> 15) == (uint32_t)sign)) hit |= 0x3F80u << (16 * u);
-                                if (key0 + 16 * t16 + (e & 3) + 8 * (e >> 2) + 4 * half < open_to) open |= 0x3F80u << (16 * u);
-                            }
-                            v[i] = number;
-                            found[i] = hit;
-                            sees[i] = open;
-                        }
-                        if (sign == 0) rows.o[d] = mfma_32x32x16_bf16(__builtin_bit_cast(v8bf, v), Block::p_operand(p, t16), rows.o[d]);
-                        count = mfma_32x32x16_bf16(__builtin_bit_cast(v8bf, found), __builtin_bit_cast(v8bf, sees), count);
-                    }
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (count[r] > 0.0f) rows.o[d][r] += sign ? NEG_INF : -NEG_INF;
-                }
-            return;
-        }
         rows.template add_values<buffer>(p);
     };
     for (int kt = 0; kt < n_tiles; kt += 2) {
         step(kt, std::integral_constant<int, 0>{});
         if (kt + 1 < n_tiles) step(kt + 1, std::integral_constant<int, 1>{});
     }
-    };
-    walk(std::false_type{});
     float none = 0.0f;                                           // NaN if any output is no number
+    if (walk == PLAIN) {
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
+        for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) none = fmaf(rows.o[d][r], 0.0f, none);
-    if (__builtin_expect(__syncthreads_or(none != 0.0f), 0)) walk(std::true_type{});
+            for (int r = 0; r < 16; ++r) none = fmaf(rows.o[d][r], 0.0f, none);
+    }
+    if (__builtin_expect(uniform(__syncthreads_or(none != 0.0f)), 0)) continue;
     // O^T to rows of bf16 through this wavefront's part of LDS (all are past the barrier above), so that whole rows go to memory
     const float inv = inverse_sum(sum_over_32(rows.l));
-    uint8_t* slab = lds + wave * 32 * ROW;
+    const uint32_t slab = lds_base + wave * 32 * ROW;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int r = 0; r < 16; r += 4)
-            *reinterpret_cast<uint2*>(slab + col * ROW + (((4 * d + (r >> 2)) ^ swizzle<D>(col)) << 4) + 8 * half) =
-                make_uint2(pack_bf16(rows.o[d][r] * inv, rows.o[d][r + 1] * inv), pack_bf16(rows.o[d][r + 2] * inv, rows.o[d][r + 3] * inv));
+            lds_write(slab + col * ROW + (uint32_t)(((4 * d + (r >> 2)) ^ swizzle<D>(col)) << 4) + 8 * half,
+                      u32x2{pack_bf16(rows.o[d][r] * inv, rows.o[d][r + 1] * inv), pack_bf16(rows.o[d][r + 2] * inv, rows.o[d][r + 3] * inv)});
     wave_lds_fence();
     constexpr bool BYTES = sizeof(OutT) == 1;
     constexpr int LANES = BYTES ? PIECES / 2 : PIECES;           // per row, 16 bytes of the output each
+    constexpr int EACH = 16 / (int)sizeof(OutT);
     const int piece = lane % LANES;
-    OutT* y = static_cast<OutT*>(a.y) + (int64_t)(seq_start + q0 + 32 * wave) * a.ldy + (int64_t)head * D + piece * (16 / (int)sizeof(OutT));
+    OutT* y = static_cast<OutT*>(a.y) + (int64_t)(seq_start + q0 + 32 * wave) * a.ldy + (int64_t)head * D + piece * EACH;
     const StaticQuantizer quant(BYTES ? *a.y_scale : 1.0f);
 #pragma unroll
     for (int n = 0; n < LANES / 2; ++n) {
         const int r = n * (64 / LANES) + lane / LANES;
-        const uint8_t* from = slab + r * ROW;
-        uint4 out;
+        const uint32_t from = slab + r * ROW;
+        u32x4 out;
         if (BYTES) {
-            const uint4 lo = *reinterpret_cast<const uint4*>(from + (((2 * piece) ^ swizzle<D>(r)) << 4));
-            const uint4 hi = *reinterpret_cast<const uint4*>(from + (((2 * piece + 1) ^ swizzle<D>(r)) << 4));
-            out = make_uint4(quant_bf16(lo.x, lo.y, quant), quant_bf16(lo.z, lo.w, quant), quant_bf16(hi.x, hi.y, quant), quant_bf16(hi.z, hi.w, quant));
+            const u32x4 lo = lds_read<u32x4>(from + (uint32_t)(((2 * piece) ^ swizzle<D>(r)) << 4));
+            const u32x4 hi = lds_read<u32x4>(from + (uint32_t)(((2 * piece + 1) ^ swizzle<D>(r)) << 4));
+            out = u32x4{quant_bf16(lo[0], lo[1], quant), quant_bf16(lo[2], lo[3], quant), quant_bf16(hi[0], hi[1], quant), quant_bf16(hi[2], hi[3], quant)};
         } else {
-            out = *reinterpret_cast<const uint4*>(from + ((piece ^ swizzle<D>(r)) << 4));
+            out = lds_read<u32x4>(from + (uint32_t)((piece ^ swizzle<D>(r)) << 4));
         }
-        if (q0 + 32 * wave + r < len) *reinterpret_cast<uint4*>(y + (int64_t)r * a.ldy) = out;
+        if (q0 + 32 * wave + r < len && walk <= NUMBERS) *reinterpret_cast<u32x4*>(y + (int64_t)r * a.ldy) = out;
+    }
+    if (__builtin_expect(walk == PLAIN, 1)) break;
+    if (walk >= PLUS) {                                          // the outputs that see an infinity or NaN become it
+        for (int i = 0; i < 16 * D / 32; ++i) {
+            const int r = i / EACH * (64 / LANES) + lane / LANES, c = piece * EACH + i % EACH;
+            const uint16_t count = lds_read<uint16_t>(slab + r * ROW + (uint32_t)(((c / 8) ^ swizzle<D>(r)) << 4) + c % 8 * 2);
+            if (count == 0 || q0 + 32 * wave + r >= len) continue;
+            OutT* at = y + (int64_t)r * a.ldy + i % EACH;
+            if (walk == PLUS) {
+                marked |= (uint64_t)1 << i;
+                *at = BYTES ? (OutT)quantize_one(-NEG_INF, quant.s) : (OutT)0x7F80;
+            } else {
+                const bool both = marked >> i & 1;
+                *at = BYTES ? (OutT)quantize_one(both ? __builtin_nanf("") : NEG_INF, quant.s) : (OutT)(both ? 0x7FC0 : 0xFF80);
+            }
+        }
+        if (walk == MINUS) break;
+    }
+    __syncthreads();                                             // all have read what the next walk's tiles replace
     }
 }
 
-template <int D, int WAVES, bool CAUSAL>
+template <int D, int WAVES, int BN, bool CAUSAL>
 void launch_tile(const PromptArgs& a, hipStream_t st) {
     const int64_t tiles = a.T / (32 * WAVES) + a.n_seqs;         // at most
     const int by_head = a.kv_heads % XCDS_A == 0;
     const dim3 grid((unsigned)(tiles * a.q_heads)), block(64 * WAVES);
-    if (a.y_scale) hipLaunchKernelGGL((attention_prompt_kernel<D, WAVES, CAUSAL, uint8_t>), grid, block, 0, st, a, (int)tiles, by_head);
-    else hipLaunchKernelGGL((attention_prompt_kernel<D, WAVES, CAUSAL, uint16_t>), grid, block, 0, st, a, (int)tiles, by_head);
+    if (a.y_scale) hipLaunchKernelGGL((attention_prompt_kernel<D, WAVES, BN, CAUSAL, uint8_t>), grid, block, 0, st, a, (int)tiles, by_head);
+    else hipLaunchKernelGGL((attention_prompt_kernel<D, WAVES, BN, CAUSAL, uint16_t>), grid, block, 0, st, a, (int)tiles, by_head);
 }
 
 }  // namespace
 
 int launch_attention_prompt(const PromptArgs& a, hipStream_t st) {
     if (a.head_dim == 128) {
-        if (a.causal) launch_tile<128, 4, true>(a, st);
-        else launch_tile<128, 4, false>(a, st);
+        if (a.causal) launch_tile<128, 4, 64, true>(a, st);
+        else launch_tile<128, 4, 64, false>(a, st);
     } else {
-        if (a.causal) launch_tile<64, 4, true>(a, st);
-        else launch_tile<64, 4, false>(a, st);
+        if (a.causal) launch_tile<64, 4, 64, true>(a, st);
+        else launch_tile<64, 4, 64, false>(a, st);
     }
     return launch_status();
 }

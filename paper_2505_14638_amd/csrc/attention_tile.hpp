@@ -7,8 +7,6 @@
 
 namespace w4a8 {
 
-constexpr int TILE_KEYS = 64;
-
 // LDS keeps rows of D bf16 in 16-byte pieces, piece p of row r at p ^ swizzle(r): eight rows next to each other have any one piece in
 // eight different bank groups (the rows a read of K touches), and four rows' 64-byte quarters lie in four (a transposing read of V).
 template <int D> __device__ __forceinline__ constexpr int swizzle(int r) {
@@ -20,8 +18,12 @@ template <typename T> __device__ __forceinline__ T lds_read(uint32_t at) {
     return *reinterpret_cast<__attribute__((address_space(3))) const T*>((uintptr_t)at);
 }
 
+template <typename T> __device__ __forceinline__ void lds_write(uint32_t at, T x) {
+    *reinterpret_cast<__attribute__((address_space(3))) T*>((uintptr_t)at) = x;
+}
+
 // LDS: two buffers of a tile of keys and the tile of values behind it.
-template <int D> struct RowBlock {
+template <int D, int TILE_KEYS = 64> struct RowBlock {
     static constexpr int ROW = 2 * D, PIECES = D / 8, TILE = TILE_KEYS * ROW, RPC = 1024 / ROW;   // RPC: rows per 64 x 16 bytes
     static constexpr int KS = D / 16, DT = D / 32, KT = TILE_KEYS / 32;
     v8bf q[KS];                                                  // Q^T, the second operand of S^T = K Q^T
