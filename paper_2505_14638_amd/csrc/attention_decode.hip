@@ -12,7 +12,6 @@
 namespace w4a8 {
 namespace {
 
-constexpr int TILE_KEYS = 64;                                    // of the prefix for many rows
 constexpr int STEP = 32, WAVES_D = 4;                           // keys of a step; wavefronts of most workgroups
 
 // N bytes of a lane's part of a row.

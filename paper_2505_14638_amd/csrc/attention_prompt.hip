@@ -88,16 +88,20 @@ __device__ __forceinline__ uint32_t seen_by(int walk, uint32_t w) {
     return r;
 }
 
-template <int D, int WAVES, int BN, bool CAUSAL, typename OutT>
-__global__ void __launch_bounds__(64 * WAVES, BN == 32 ? 3 : 2) attention_prompt_kernel(PromptArgs a, int tiles, int by_head) {
-    using Block = RowBlock<D, BN>;
-    constexpr int BM = 32 * WAVES, ROW = Block::ROW, PIECES = Block::PIECES, TILE = Block::TILE, RPC = Block::RPC;
+// SHARE wavefronts share 32 rows and take a part of every tile's keys each.
+template <int D, int SHARE, bool CAUSAL, typename OutT>
+__global__ void __launch_bounds__(256, 2) attention_prompt_kernel(PromptArgs a, int tiles, int by_head) {
+    constexpr int WAVES = 4, BN = TILE_KEYS, KEYS = BN / SHARE;
+    using Block = RowBlock<D, KEYS>;
+    constexpr int BM = 32 * WAVES / SHARE, ROW = Block::ROW, PIECES = Block::PIECES, TILE = Block::TILE, RPC = Block::RPC;
     constexpr int DT = Block::DT, KT = Block::KT;
     constexpr int COPIES = TILE / 1024 / WAVES;                  // of 64 lanes x 16 bytes, per wavefront for each of K and V
-    // K 0, V 0, K 1, V 1; first Q, from K 1 on; at last O, from K 0 on
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * TILE + (2 * TILE > BM * ROW ? 2 * TILE : BM * ROW)];
+    // K 0, V 0, K 1, V 1; first Q, from K 1 on; at last O, from K 0 on, and behind it what is to be joined
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * TILE];
+    static_assert(BM * ROW <= 2 * TILE && (SHARE == 1 || BM * ROW + BM * (2 * ROW + 8) <= 4 * TILE), "what goes there");
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
+    const int band = wave / SHARE, part = wave % SHARE;          // this wavefront's 32 rows and keys of a tile
     const int group = a.q_heads / a.kv_heads;
 
     // by_head: every XCD keeps to its own key heads, whose keys and values then stay in its L2; a tile's query heads that share a
@@ -116,7 +120,7 @@ __global__ void __launch_bounds__(64 * WAVES, BN == 32 ? 3 : 2) attention_prompt
     const int kv_head = head / group;
     int seq_start, len, tile;
     if (!find_tile<BM>(a.starts, a.n_seqs, a.T, t, seq_start, len, tile)) return;
-    const int q0 = tile * BM, row = q0 + 32 * wave + col;        // this lane's row of the sequence
+    const int q0 = tile * BM, row = q0 + 32 * band + col;        // this lane's row of the sequence
     const int key_end = CAUSAL ? min(len, q0 + BM) : len;
     const int n_tiles = (key_end + BN - 1) / BN;
 
@@ -161,18 +165,18 @@ __global__ void __launch_bounds__(64 * WAVES, BN == 32 ? 3 : 2) attention_prompt
             }
         }
     };
-    Block rows(lds_base, lane);
+    Block rows(lds_base, lane, KEYS * part);
     {
         const uint8_t* from = reinterpret_cast<const uint8_t*>(a.q + (int64_t)(seq_start + q0) * a.ldq + (int64_t)head * D);
 #pragma unroll
         for (int q = 0; q < 32 / RPC; ++q) {
-            const int r = 32 * wave + q * RPC + lane / PIECES;
+            const int r = 32 * band + q * RPC + lane / PIECES;
             lds_dma_16(from, (uint32_t)min(r, len - 1 - q0) * (uint32_t)(a.ldq * 2) + (uint32_t)(((lane % PIECES) ^ swizzle<D>(r)) * 16),
-                       lds_base + 2 * TILE + (32 * wave + q * RPC) * ROW);
+                       lds_base + 2 * TILE + (32 * band + q * RPC) * ROW);
         }
         copy_tile(0, 0);                                         // on its way together with them
-        lds_dma_wait_all();                                      // a wavefront copies its own rows
-        rows.read_q(2 * TILE + wave * 32 * ROW);
+        lds_dma_wait_all();                                      // a wavefront copies its own rows (those that share them, the same bytes)
+        rows.read_q(2 * TILE + (32 * band - KEYS * part) * ROW);
     }
 
     // A weight of zero takes a key out of the sums, unless its value is no number.  So if an output is none, the rows are walked again with zeros
@@ -186,8 +190,8 @@ __global__ void __launch_bounds__(64 * WAVES, BN == 32 ? 3 : 2) attention_prompt
         lds_dma_wait_all();
         __syncthreads();
         if (kt + 1 < n_tiles) copy_tile(kt + 1, buffer ^ 1);
-        const int key0 = kt * BN;
-        if (CAUSAL && key0 > q0 + 32 * wave + 31) return;        // (wave-uniform) no row of this wavefront sees the tile
+        const int key0 = kt * BN + KEYS * part;
+        if (CAUSAL && key0 > q0 + 32 * band + 31) return;        // (wave-uniform) no row of this wavefront sees its keys of the tile
         v16f s[KT];
         rows.template scores<buffer>(s);
         for (int counts = uniform(walk >= PLUS); counts;) {      // (a loop of at most one pass, as below)
@@ -197,7 +201,7 @@ __global__ void __launch_bounds__(64 * WAVES, BN == 32 ? 3 : 2) attention_prompt
                 for (int r = 0; r < 16; ++r) s[k][r] = 0.0f;
             asm volatile("s_mov_b32 %0, 0" : "=s"(counts));
         }
-        const bool masked = key0 + BN > len || (CAUSAL && key0 + BN - 1 > q0 + 32 * wave);
+        const bool masked = key0 + KEYS > len || (CAUSAL && key0 + KEYS - 1 > q0 + 32 * band);
         const int seen = CAUSAL ? min(len, row + 1) : len;       // keys below this one
         // a loop of at most one pass: as a branch the compiler turns it into 32 comparisons and selects in every tile
         int hides = uniform(masked);
@@ -228,8 +232,36 @@ __global__ void __launch_bounds__(64 * WAVES, BN == 32 ? 3 : 2) attention_prompt
     }
     if (__builtin_expect(uniform(__syncthreads_or(none != 0.0f)), 0)) continue;
     // O^T to rows of bf16 through this wavefront's part of LDS (all are past the barrier above), so that whole rows go to memory
-    const float inv = inverse_sum(sum_over_32(rows.l));
-    const uint32_t slab = lds_base + wave * 32 * ROW;
+    float total = sum_over_32(rows.l);
+    if (SHARE == 2) {                                            // the two halves of the keys joined, by the wavefront of the first
+        const uint32_t theirs = lds_base + BM * ROW + band * 32 * (2 * ROW + 8) + lane * 16, ml = theirs + 32 * 2 * ROW - lane * 8;
+        if (part == 1) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4)
+                    lds_write(theirs + (d * 4 + r / 4) * 1024, v4f{rows.o[d][r], rows.o[d][r + 1], rows.o[d][r + 2], rows.o[d][r + 3]});
+            if (half == 0) lds_write(ml, v2f{rows.m, total});
+        }
+        __syncthreads();
+        if (part == 0) {
+            const v2f other = lds_read<v2f>(half ? ml - 256 : ml);
+            const float top = fmaxf(rows.m, other[0]);
+            const float mine = rows.m == NEG_INF ? 0.0f : exp2_fast(rows.m - top), more = other[0] == NEG_INF ? 0.0f : exp2_fast(other[0] - top);
+            total = fmaf(total, mine, other[1] * more);
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const v4f x = lds_read<v4f>(theirs + (d * 4 + r / 4) * 1024);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) rows.o[d][r + i] = fmaf(rows.o[d][r + i], mine, x[i] * more);
+                }
+        }
+    }
+    const float inv = inverse_sum(total);
+    const uint32_t slab = lds_base + band * 32 * ROW;
+    if (part == 0) {
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -241,7 +273,7 @@ __global__ void __launch_bounds__(64 * WAVES, BN == 32 ? 3 : 2) attention_prompt
     constexpr int LANES = BYTES ? PIECES / 2 : PIECES;           // per row, 16 bytes of the output each
     constexpr int EACH = 16 / (int)sizeof(OutT);
     const int piece = lane % LANES;
-    OutT* y = static_cast<OutT*>(a.y) + (int64_t)(seq_start + q0 + 32 * wave) * a.ldy + (int64_t)head * D + piece * EACH;
+    OutT* y = static_cast<OutT*>(a.y) + (int64_t)(seq_start + q0 + 32 * band) * a.ldy + (int64_t)head * D + piece * EACH;
     const StaticQuantizer quant(BYTES ? *a.y_scale : 1.0f);
 #pragma unroll
     for (int n = 0; n < LANES / 2; ++n) {
@@ -255,14 +287,13 @@ __global__ void __launch_bounds__(64 * WAVES, BN == 32 ? 3 : 2) attention_prompt
         } else {
             out = lds_read<u32x4>(from + (uint32_t)((piece ^ swizzle<D>(r)) << 4));
         }
-        if (q0 + 32 * wave + r < len && walk <= NUMBERS) *reinterpret_cast<u32x4*>(y + (int64_t)r * a.ldy) = out;
+        if (q0 + 32 * band + r < len && walk <= NUMBERS) *reinterpret_cast<u32x4*>(y + (int64_t)r * a.ldy) = out;
     }
-    if (__builtin_expect(walk == PLAIN, 1)) break;
     if (walk >= PLUS) {                                          // the outputs that see an infinity or NaN become it
         for (int i = 0; i < 16 * D / 32; ++i) {
             const int r = i / EACH * (64 / LANES) + lane / LANES, c = piece * EACH + i % EACH;
             const uint16_t count = lds_read<uint16_t>(slab + r * ROW + (uint32_t)(((c / 8) ^ swizzle<D>(r)) << 4) + c % 8 * 2);
-            if (count == 0 || q0 + 32 * wave + r >= len) continue;
+            if (count == 0 || q0 + 32 * band + r >= len) continue;
             OutT* at = y + (int64_t)r * a.ldy + i % EACH;
             if (walk == PLUS) {
                 marked |= (uint64_t)1 << i;
@@ -272,30 +303,43 @@ __global__ void __launch_bounds__(64 * WAVES, BN == 32 ? 3 : 2) attention_prompt
                 *at = BYTES ? (OutT)quantize_one(both ? __builtin_nanf("") : NEG_INF, quant.s) : (OutT)(both ? 0x7FC0 : 0xFF80);
             }
         }
-        if (walk == MINUS) break;
     }
+    }
+    if (walk == PLAIN || walk == MINUS) break;
     __syncthreads();                                             // all have read what the next walk's tiles replace
     }
 }
 
-template <int D, int WAVES, int BN, bool CAUSAL>
+template <int D, int SHARE, bool CAUSAL>
 void launch_tile(const PromptArgs& a, hipStream_t st) {
-    const int64_t tiles = a.T / (32 * WAVES) + a.n_seqs;         // at most
+    constexpr int BM = 128 / SHARE;
+    const int64_t tiles = a.n_seqs == 1 ? (a.T + BM - 1) / BM : a.T / BM + a.n_seqs;   // at most
     const int by_head = a.kv_heads % XCDS_A == 0;
-    const dim3 grid((unsigned)(tiles * a.q_heads)), block(64 * WAVES);
-    if (a.y_scale) hipLaunchKernelGGL((attention_prompt_kernel<D, WAVES, BN, CAUSAL, uint8_t>), grid, block, 0, st, a, (int)tiles, by_head);
-    else hipLaunchKernelGGL((attention_prompt_kernel<D, WAVES, BN, CAUSAL, uint16_t>), grid, block, 0, st, a, (int)tiles, by_head);
+    const dim3 grid((unsigned)(tiles * a.q_heads)), block(256);
+    if (a.y_scale) hipLaunchKernelGGL((attention_prompt_kernel<D, SHARE, CAUSAL, uint8_t>), grid, block, 0, st, a, (int)tiles, by_head);
+    else hipLaunchKernelGGL((attention_prompt_kernel<D, SHARE, CAUSAL, uint16_t>), grid, block, 0, st, a, (int)tiles, by_head);
+}
+
+// Workgroups of 128 rows read least; but a wavefront's way through a tile is one chain of instructions that wait for each other, and with
+// hardly more than one workgroup per compute unit nothing else fills those waits.  Then 64 rows a workgroup, two wavefronts on each 32: one
+// prompt of 512 tokens, 32 heads, 14.2 -> 13.2 us (128 workgroups of 128 rows), of 1100 27.1 -> 24.3 (288), of 2000 on 8 heads of 64 channels
+// 28.9 -> 22.7 (128).  Three of 700 .. 1500 on 16 heads of 64 channels (432) lose, 37 -> 44.
+constexpr int FEW = 384;
+template <int D, bool CAUSAL>
+void launch_rows(const PromptArgs& a, hipStream_t st) {
+    if ((a.T + 127) / 128 * a.q_heads <= FEW) launch_tile<D, 2, CAUSAL>(a, st);
+    else launch_tile<D, 1, CAUSAL>(a, st);
 }
 
 }  // namespace
 
 int launch_attention_prompt(const PromptArgs& a, hipStream_t st) {
     if (a.head_dim == 128) {
-        if (a.causal) launch_tile<128, 4, 64, true>(a, st);
-        else launch_tile<128, 4, 64, false>(a, st);
+        if (a.causal) launch_rows<128, true>(a, st);
+        else launch_rows<128, false>(a, st);
     } else {
-        if (a.causal) launch_tile<64, 4, 64, true>(a, st);
-        else launch_tile<64, 4, 64, false>(a, st);
+        if (a.causal) launch_rows<64, true>(a, st);
+        else launch_rows<64, false>(a, st);
     }
     return launch_status();
 }

@@ -22,10 +22,12 @@ template <typename T> __device__ __forceinline__ void lds_write(uint32_t at, T x
     *reinterpret_cast<__attribute__((address_space(3))) T*>((uintptr_t)at) = x;
 }
 
-// LDS: two buffers of a tile of keys and the tile of values behind it.
-template <int D, int TILE_KEYS = 64> struct RowBlock {
+constexpr int TILE_KEYS = 64;
+
+// LDS: two buffers of a tile of keys and the tile of values behind it, of which the wavefront takes KEYS keys from key `first` on.
+template <int D, int KEYS = TILE_KEYS> struct RowBlock {
     static constexpr int ROW = 2 * D, PIECES = D / 8, TILE = TILE_KEYS * ROW, RPC = 1024 / ROW;   // RPC: rows per 64 x 16 bytes
-    static constexpr int KS = D / 16, DT = D / 32, KT = TILE_KEYS / 32;
+    static constexpr int KS = D / 16, DT = D / 32, KT = KEYS / 32;
     v8bf q[KS];                                                  // Q^T, the second operand of S^T = K Q^T
     v16f o[DT];                                                  // O^T: channel 32 d + (r & 3) + 8 (r >> 2) + 4 half of row lane % 32
     float m, l;                                                  // the maximum that the sums go by (scaled, base 2), this lane's part of the sum
@@ -33,16 +35,16 @@ template <int D, int TILE_KEYS = 64> struct RowBlock {
     // + {0..3} and 8 more, 16 channels per 16 lanes
     uint32_t k_addr[KS], v_addr[DT][2];
 
-    __device__ __forceinline__ RowBlock(uint32_t lds, int lane) {
+    __device__ __forceinline__ RowBlock(uint32_t lds, int lane, int first = 0) {
         const int col = lane & 31, half = lane >> 5, j = lane & 15, g1 = (lane >> 4) & 1;
 #pragma unroll
-        for (int i = 0; i < KS; ++i) k_addr[i] = lds + col * ROW + (uint32_t)(((half ^ swizzle<D>(col)) ^ (2 * i)) << 4);
+        for (int i = 0; i < KS; ++i) k_addr[i] = lds + (first + col) * ROW + (uint32_t)(((half ^ swizzle<D>(col)) ^ (2 * i)) << 4);
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int r = 4 * half + (j >> 2), piece = 2 * g1 + ((j & 3) >> 1);
-                v_addr[d][e] = lds + TILE + (r + 8 * e) * ROW + (j & 1) * 8 + (uint32_t)((piece ^ swizzle<D>(r) ^ (4 * d) ^ (2 * e)) << 4);
+                v_addr[d][e] = lds + TILE + (first + r + 8 * e) * ROW + (j & 1) * 8 + (uint32_t)((piece ^ swizzle<D>(r) ^ (4 * d) ^ (2 * e)) << 4);
             }
     }
     __device__ __forceinline__ void clear() {
@@ -58,7 +60,7 @@ template <int D, int TILE_KEYS = 64> struct RowBlock {
 #pragma unroll
         for (int i = 0; i < KS; ++i) q[i] = lds_read<v8bf>(k_addr[i] + at);
     }
-    // s[k][r]: key 32 k + (r & 3) + 8 (r >> 2) + 4 half of the tile
+    // s[k][r]: key first + 32 k + (r & 3) + 8 (r >> 2) + 4 half of the tile
     template <int BUFFER> __device__ __forceinline__ void scores(v16f (&s)[KT]) const {
 #pragma unroll
         for (int k = 0; k < KT; ++k) {
@@ -112,7 +114,7 @@ template <int D, int TILE_KEYS = 64> struct RowBlock {
     }
     template <int BUFFER> __device__ __forceinline__ void add_values(const uint32_t (&p)[KT][8]) {
 #pragma unroll
-        for (int t16 = 0; t16 < TILE_KEYS / 16; ++t16)
+        for (int t16 = 0; t16 < KEYS / 16; ++t16)
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d] = mfma_32x32x16_bf16(__builtin_bit_cast(v8bf, v_operand<BUFFER>(t16, d)), p_operand(p, t16), o[d]);
     }
