@@ -127,7 +127,7 @@ __device__ __forceinline__ void stream_keys(const DecodeArgs& a, const DecodePla
             for (int r = 0; r < 4; ++r) x.v[4 * kt + r] = *reinterpret_cast<const Piece<S::VB>*>(vp + (4 * kg + r) * S::ROW + S::VB * c);
         }
     };
-    auto compute = [&](const S& x, int64_t key, const bool (&ok)[2]) {
+    auto compute = [&](S& x, int64_t key, const bool (&ok)[2]) {
         v4f s[2];
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
@@ -144,13 +144,18 @@ __device__ __forceinline__ void stream_keys(const DecodeArgs& a, const DecodePla
                 s[kt] = mfma_16x16x32_bf16(kf, qf[i], s[kt]);
             }
         }
-        const bool whole = key + STEP <= k_end && ok[0] && ok[1];
-        bool seen[8];
+        // what no row sees may hold anything and counts as zero (a loop of at most one pass: as a branch it would cost every step)
+        int hides = uniform(!(key + STEP <= k_end && ok[0] && ok[1]));
+        while (hides) {
+            int64_t left = k_end - key - 4 * kg;
+            asm volatile("" : "+v"(left));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int kt = i / 4, r = i % 4;
-            seen[i] = whole || (ok[kt] && key + 16 * kt + 4 * kg + r < k_end);
-            if (!seen[i]) s[kt][r] = NEG_INF;
+            for (int i = 0; i < 8; ++i)
+                if (!ok[i / 4] || 16 * (i / 4) + i % 4 >= left) {
+                    s[i / 4][i % 4] = NEG_INF;
+                    x.v[i] = Piece<S::VB>{};
+                }
+            asm volatile("s_mov_b32 %0, 0" : "=s"(hides));
         }
         float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
         mx = max_over_32(max_over_16(mx)) * score_scale;
@@ -169,16 +174,14 @@ __device__ __forceinline__ void stream_keys(const DecodeArgs& a, const DecodePla
             l += p[i];
         }
         const v8bf pf = __builtin_bit_cast(v8bf, u32x4{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])});
-        // values as bf16 pairs of channels; what no row sees may hold anything and counts as zero
+        // values as bf16 pairs of channels
         uint32_t v[8][VD / 2];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int j = 0; j < VD / 2; ++j) {
-                uint32_t w;
-                if (E4M3) w = j & 1 ? e4m3_to_bf16<true>(x.v[i].w[j / 2]) : e4m3_to_bf16<false>(x.v[i].w[j / 2]);
-                else w = x.v[i].w[j];
-                v[i][j] = seen[i] ? w : 0u;
+                if (E4M3) v[i][j] = j & 1 ? e4m3_to_bf16<true>(x.v[i].w[j / 2]) : e4m3_to_bf16<false>(x.v[i].w[j / 2]);
+                else v[i][j] = x.v[i].w[j];
             }
 #pragma unroll
         for (int j = 0; j < VD; ++j) {
