@@ -48,6 +48,10 @@ __device__ __forceinline__ float sum_over_16(float x) {
     return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
+// A store that does not stay in L2: what a kernel leaves there is written back at its end, which then waits for it.  16 pages of 64 planes, 32
+// KB each, copied 17.3 -> 11.6 us, 400 pages 347 -> 318; ten packed prompts of 1024 tokens 118 -> 110.  (Partial results gain nothing by it.)
+template <typename T> __device__ __forceinline__ void stream_out(void* p, T x) { __builtin_nontemporal_store(x, static_cast<T*>(p)); }
+
 // Sum of the two bf16 in w, added to c.
 __device__ __forceinline__ float add_pair(uint32_t w, float c) {
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, w), __builtin_bit_cast(v2bf, 0x3F803F80u), c, false);

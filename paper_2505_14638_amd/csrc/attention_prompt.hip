@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(256, 2) attention_prompt_kernel(PromptArgs a, 
         } else {
             out = lds_read<u32x4>(from + (uint32_t)((piece ^ swizzle<D>(r)) << 4));
         }
-        if (q0 + 32 * band + r < len && walk <= NUMBERS) *reinterpret_cast<u32x4*>(y + (int64_t)r * a.ldy) = out;
+        if (q0 + 32 * band + r < len && walk <= NUMBERS) stream_out(y + (int64_t)r * a.ldy, out);
     }
     if (walk >= PLUS) {                                          // the outputs that see an infinity or NaN become it
         for (int i = 0; i < 16 * D / 32; ++i) {

@@ -8,18 +8,17 @@ namespace {
 // Sixteen channels of one head of one token: two chunks of eight, which turn together in the halves form (i with i + D/2) and lie
 // side by side in the pairs form (2i with 2i + 1).
 struct Channels {
-    uint4 lo, hi;
+    u32x4 lo, hi;
 };
-__device__ __forceinline__ void unpack(uint4 a, float (&x)[8]) {
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+__device__ __forceinline__ void unpack(u32x4 w, float (&x)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         x[2 * i] = __uint_as_float(w[i] << 16);
         x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
     }
 }
-__device__ __forceinline__ uint4 pack(const float (&x)[8]) {
-    return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+__device__ __forceinline__ u32x4 pack(const float (&x)[8]) {
+    return u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
 }
 
 // (a, b) -> (a cos - b sin, b cos + a sin) in float32, eight times.
@@ -77,8 +76,8 @@ __global__ void __launch_bounds__(256) rope_cache_write_kernel(RopeCacheArgs a, 
         const int h = first + j * step;
         if (h < heads) {
             const uint16_t* p = a.qkv + t * a.ldqkv + (int64_t)h * D;
-            x[j].lo = *reinterpret_cast<const uint4*>(p + d_lo);
-            x[j].hi = *reinterpret_cast<const uint4*>(p + d_hi);
+            x[j].lo = *reinterpret_cast<const u32x4*>(p + d_lo);
+            x[j].hi = *reinterpret_cast<const u32x4*>(p + d_hi);
         }
     }
     const int64_t page = slot >> a.c.page_shift, off = slot & (a.c.page_size - 1);
@@ -95,8 +94,8 @@ __global__ void __launch_bounds__(256) rope_cache_write_kernel(RopeCacheArgs a, 
                             : a.k_out     ? a.k_out + t * a.ldk + (int64_t)(h - a.q_heads) * D
                                           : nullptr;
             if (out) {
-                *reinterpret_cast<uint4*>(out + d_lo) = pack(lo);
-                *reinterpret_cast<uint4*>(out + d_hi) = pack(hi);
+                stream_out(out + d_lo, pack(lo));
+                stream_out(out + d_hi, pack(hi));
             }
         }
         if (h >= a.q_heads) {
@@ -106,12 +105,12 @@ __global__ void __launch_bounds__(256) rope_cache_write_kernel(RopeCacheArgs a, 
             uint8_t* cache = key ? a.k_cache : a.v_cache;
             if (E4M3) {
                 const StaticQuantizer q(a.kv_scales[key ? 0 : 1]);
-                *reinterpret_cast<uint2*>(cache + at + d_lo) = make_uint2(q.four(lo[0], lo[1], lo[2], lo[3]), q.four(lo[4], lo[5], lo[6], lo[7]));
-                *reinterpret_cast<uint2*>(cache + at + d_hi) = make_uint2(q.four(hi[0], hi[1], hi[2], hi[3]), q.four(hi[4], hi[5], hi[6], hi[7]));
+                stream_out(cache + at + d_lo, u32x2{q.four(lo[0], lo[1], lo[2], lo[3]), q.four(lo[4], lo[5], lo[6], lo[7])});
+                stream_out(cache + at + d_hi, u32x2{q.four(hi[0], hi[1], hi[2], hi[3]), q.four(hi[4], hi[5], hi[6], hi[7])});
             } else {
                 uint16_t* row = reinterpret_cast<uint16_t*>(cache) + at;
-                *reinterpret_cast<uint4*>(row + d_lo) = key ? pack(lo) : x[j].lo;
-                *reinterpret_cast<uint4*>(row + d_hi) = key ? pack(hi) : x[j].hi;
+                stream_out(row + d_lo, key ? pack(lo) : x[j].lo);
+                stream_out(row + d_hi, key ? pack(hi) : x[j].hi);
             }
         }
     }
@@ -130,13 +129,13 @@ __global__ void __launch_bounds__(256) cache_copy_pages_kernel(uint8_t* cache, i
     const uint8_t* s = plane + from * page_stride + begin;
     uint8_t* d = plane + to * page_stride + begin;
     if (begin + (COPY_PIECES - 1) * 4096 < page_bytes) {
-        uint4 v[COPY_PIECES];
+        u32x4 v[COPY_PIECES];
 #pragma unroll
-        for (int j = 0; j < COPY_PIECES; ++j) v[j] = *reinterpret_cast<const uint4*>(s + j * 4096);
+        for (int j = 0; j < COPY_PIECES; ++j) v[j] = *reinterpret_cast<const u32x4*>(s + j * 4096);
 #pragma unroll
-        for (int j = 0; j < COPY_PIECES; ++j) *reinterpret_cast<uint4*>(d + j * 4096) = v[j];
+        for (int j = 0; j < COPY_PIECES; ++j) stream_out(d + j * 4096, v[j]);
     } else {
-        for (int j = 0; begin + j * 4096 < page_bytes; ++j) *reinterpret_cast<uint4*>(d + j * 4096) = *reinterpret_cast<const uint4*>(s + j * 4096);
+        for (int j = 0; begin + j * 4096 < page_bytes; ++j) stream_out(d + j * 4096, *reinterpret_cast<const u32x4*>(s + j * 4096));
     }
 }
 
