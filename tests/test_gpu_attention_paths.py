@@ -1,0 +1,213 @@
+"""Attention and its cache where calls are large or far apart: the kernels that only many rows reach, tensors beyond 32 bits of bytes, other
+streams, calls at the same time, captured calls."""
+import math
+
+import pytest
+import torch
+
+import attention_reference as R
+from paper_2505_14638_amd import binding as B
+from test_gpu_attention import DEV, ints, paged, prompt_inputs, randn
+
+pytestmark = pytest.mark.gpu
+
+
+def bounds(lengths, lead=0):
+    return [lead + sum(lengths[:i]) for i in range(len(lengths) + 1)]
+
+
+# Many rows (tiles of 128 times heads above a few hundred) have four wavefronts on rows of their own, few have pairs on the same rows.
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lengths,hq,hk,d", [
+    ([600], 96, 8, 128), ([100, 0, 1, 260, 64], 128, 16, 64), ([129, 127, 128, 33], 112, 7, 128), ([321, 320], 90, 1, 64),
+    ([(37 * i) % 23 for i in range(90)], 64, 4, 64),
+])
+def test_prompt_of_many_rows(gpu_lib, lengths, hq, hk, d, causal):
+    starts = bounds(lengths)
+    t = starts[-1]
+    assert -(-t // 128) * hq > 384
+    q, k, v = prompt_inputs(5 * t + hq, t, hq, hk, d)
+    y = B.attention_prompt(q, k, v, ints(starts), causal=causal)
+    out, size = R.prompt(q, k, v, starts, d, causal)
+    assert R.worst(y, out, size) <= 1.0
+    scale = torch.tensor([0.013], device=DEV)
+    assert torch.equal(B.attention_prompt(q, k, v, ints(starts), causal=causal, y_scale=scale), B.quantize_act(y, scale))
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("t,hq,hk,d", [(900, 64, 2, 128), (900, 64, 2, 64), (400, 4, 2, 128), (400, 4, 2, 64)])
+def test_values_that_are_no_numbers(gpu_lib, t, hq, hk, d, causal):
+    """Infinities of both signs and NaN among the values reach the rows that see them, in their channel and their heads, and nothing else."""
+    q, k, v = prompt_inputs(31, t, hq, hk, d)
+    v = v.clone()
+    y = B.attention_prompt(q, k, v, ints([0, t]), causal=causal).view(t, hk, hq // hk, d)
+    plus, minus, none, lone = 100, 230, 333, 65
+    bad = v.clone()
+    bad[plus, 1, 5], bad[minus, 1, 5] = math.inf, -math.inf      # NaN where both are seen
+    bad[none, 1, 6], bad[lone, 1, d - 1] = math.nan, -math.inf
+    want = y.clone()
+    at = (lambda i: i) if causal else (lambda i: 0)              # the first row that sees key i
+    want[at(plus):, 1, :, 5] = math.inf
+    want[max(at(plus), at(minus)):, 1, :, 5] = math.nan
+    want[at(none):, 1, :, 6] = math.nan
+    want[at(lone):, 1, :, d - 1] = -math.inf
+    got = B.attention_prompt(q, k, bad, ints([0, t]), causal=causal)
+    same = got.view_as(want)
+    assert torch.equal(torch.isnan(same), torch.isnan(want))
+    assert torch.equal(same.nan_to_num(7.0, math.inf, -math.inf), want.nan_to_num(7.0, math.inf, -math.inf))
+    scale = torch.tensor([0.02], device=DEV)
+    assert torch.equal(B.attention_prompt(q, k, bad, ints([0, t]), causal=causal, y_scale=scale), B.quantize_act(got, scale))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_decode_of_sequences_of_very_different_lengths(gpu_lib, cache):
+    """One workgroup on thousands of tokens, whose page numbers it lists more than once, beside others on a few or none."""
+    lengths, hq, hk, d, page = [9000, 4097, 0, 4096] + [(11 * i) % 50 for i in range(60)], 8, 8, 64, 16
+    k, v, scales, tables, _ = paged(2, lengths, 0, hk, d, page, cache, fill=math.nan if cache == "bf16" else None)
+    q = randn(5, len(lengths), hq, d).bfloat16()
+    y = B.attention_decode(q, k, v, ints(tables), ints(lengths), kv_scales=scales)
+    k_scale, v_scale = (None, None) if scales is None else scales.tolist()
+    out, size = R.decode(q, R.cache_values(k, k_scale), R.cache_values(v, v_scale), tables, lengths, d)
+    assert R.worst(y, out, size) <= 1.0
+
+
+@pytest.mark.parametrize("n", [2, 20])
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_cache_beyond_32_bits(gpu_lib, kind, n):
+    """Pages 2^27 elements apart, forty of them: written, copied and read where an offset in 32 bits would end elsewhere."""
+    hq, hk, d, page, n_pages, far = 8, 2, 128, 16, 40, 1 << 27
+    dtype = torch.bfloat16 if kind == "bf16" else torch.uint8
+    pool = torch.empty(n_pages * far, dtype=dtype, device=DEV)
+    k, v = (pool.as_strided((n_pages, hk, page, d), (far, page * d, d, 1), o) for o in (0, hk * page * d))
+    k.zero_(), v.zero_()
+    scales = torch.tensor([0.011, 0.017], device=DEV) if kind == "e4m3" else None
+    prefix, own = 64, 40                                         # tokens: pages 39 .. 36, then pages 35, 3, 34 of the first sequence
+    prefix_pages, table = [39, 38, 37, 36], [35, 3, 34]
+    t = prefix + own
+    qkv = randn(3, t, (hq + 2 * hk) * d).bfloat16()
+    places = [p * page + i for p in prefix_pages + table for i in range(page)][:t]
+    cos_sin = torch.cat([torch.ones(1, d // 2), torch.zeros(1, d // 2)], dim=1).to(DEV)   # no turn: the cache holds the rows
+    q = B.rope_cache_write(qkv, cos_sin, ints([0] * t), ints(places), k, v, kv_scales=scales)
+    rows = R.heads(qkv, d)
+    assert torch.equal(q, qkv[:, :hq * d])
+    near = {p: i for i, p in enumerate(prefix_pages + table)}
+    kk, vv = (torch.stack([x[p] for p in prefix_pages + table]) for x in (k, v))
+    if kind == "bf16":
+        written = kk.permute(0, 2, 1, 3).flatten(0, 1)[:t].cpu().double()
+        assert torch.equal(written, rows[:, hq:hq + hk])
+    q = randn(4, n, hq, d).bfloat16()
+    tables = [table] + [[table[i % 3]] * 3 for i in range(n - 1)]
+    lengths = [own] + [(7 * i) % 48 for i in range(n - 1)]
+    args = dict(prefix_pages=ints(prefix_pages), prefix_length=prefix, kv_scales=scales)
+    y = B.attention_decode(q, k, v, ints(tables), ints(lengths), **args)
+    k_scale, v_scale = (None, None) if scales is None else scales.tolist()
+    out, size = R.decode(q, R.cache_values(kk, k_scale), R.cache_values(vv, v_scale), [[near[p] for p in x] for x in tables], lengths, d,
+                         [near[p] for p in prefix_pages], prefix)
+    assert R.worst(y, out, size) <= 1.0
+    # each page of the prefix and of the first sequence to a page near the start
+    src, dst = prefix_pages + table, [0, 1, 2, 4, 5, 6, 7]
+    B.cache_copy_pages(pool.as_strided((1, n_pages, 2 * hk, page, d), (0, far, page * d, d, 1)), ints(src), ints(dst))
+    args["prefix_pages"] = ints(dst[:4])
+    moved = [[dst[src.index(p)] for p in x] for x in tables]
+    assert torch.equal(B.attention_decode(q, k, v, ints(moved), ints(lengths), **args), y)
+    assert (k[8:34] == 0).all() and (v[8:34] == 0).all()
+
+
+def test_prompt_rows_beyond_32_bits(gpu_lib):
+    t, hq, hk, d, wide = 2200, 2, 1, 64, (1 << 20) - 8
+    x = torch.empty((t, wide), dtype=torch.bfloat16, device=DEV)     # 4.6 GB
+    q, k, v = prompt_inputs(6, t, hq, hk, d)
+    far = [x[:, 0:128].unflatten(1, (hq, d)), x[:, 128:192].unflatten(1, (hk, d)), x[:, wide - 64:].unflatten(1, (hk, d))]
+    for a, b in zip(far, (q, k, v)):
+        a.copy_(b)
+    y = B.attention_prompt(*far, ints([0, 9, t]), out=x[:, 512:640])
+    assert torch.equal(y, B.attention_prompt(q, k, v, ints([0, 9, t])))
+
+
+def test_calls_at_the_same_time_on_two_streams(gpu_lib):
+    """Each with its own workspace; the tensors were made on another stream."""
+    hq, hk, d, page = 32, 8, 128, 16
+    calls = []
+    for seed, lengths, prefix in ((1, [900, 40], 0), (2, [70] * 30, 500)):
+        k, v, _, tables, prefix_pages = paged(seed, lengths, prefix, hk, d, page, "bf16")
+        q = randn(seed, len(lengths), hq, d).bfloat16()
+        size = B.attention_decode_workspace_bytes(len(lengths), hq, hk, d, page, len(tables[0]), prefix)
+        assert size > 0
+        calls.append((q, k, v, ints(tables), ints(lengths), dict(
+            prefix_pages=ints(prefix_pages) if prefix else None, prefix_length=prefix,
+            workspace=torch.empty(size, dtype=torch.uint8, device=DEV), out=torch.zeros((len(lengths), hq * d), dtype=torch.bfloat16, device=DEV))))
+    q, k, v = prompt_inputs(8, 300, 4, 2, 64)
+    want_prompt = B.attention_prompt(q, k, v, ints([0, 300]))
+    starts = ints([0, 300])
+    want = [B.attention_decode(*c[:5], **c[5]).clone() for c in calls]
+    for c in calls:
+        c[5]["out"].zero_()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(8):
+        for s, c in zip(streams, calls):
+            with torch.cuda.stream(s):
+                B.attention_decode(*c[:5], **c[5])
+                y = B.attention_prompt(q, k, v, starts)
+    torch.cuda.synchronize()
+    assert all(torch.equal(c[5]["out"], w) for c, w in zip(calls, want)) and torch.equal(y, want_prompt)
+
+
+def test_two_graphs_share_a_workspace(gpu_lib):
+    """Replayed one after the other, in any order: nothing of a call is left for the next."""
+    hq, hk, d, page, graphs = 8, 2, 128, 16, []
+    sets = []
+    for seed, lengths, prefix in ((1, [900, 40], 0), (2, [70, 0] * 10, 500)):
+        k, v, _, tables, prefix_pages = paged(seed, lengths, prefix, hk, d, page, "bf16")
+        sets.append((randn(seed, len(lengths), hq, d).bfloat16(), k, v, ints(tables), ints(lengths), ints(prefix_pages) if prefix else None, prefix))
+    need = [B.attention_decode_workspace_bytes(len(s[4]), hq, hk, d, page, s[3].shape[1], s[6]) for s in sets]
+    work = torch.full((max(need),), 255, dtype=torch.uint8, device=DEV)  # NaN, were it read
+    want = [B.attention_decode(*s) for s in sets]
+    outs = [torch.zeros_like(w) for w in want]
+    torch.cuda.synchronize()
+    for s, y in zip(sets, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            B.attention_decode(*s, workspace=work, out=y)
+        graphs.append(g)
+    for i in (0, 1, 1, 0, 1, 0):
+        outs[i].zero_()
+        work.fill_(255)
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[i], want[i])
+
+
+def test_captured_prompt_follows_its_inputs(gpu_lib):
+    """Rotation, cache write and attention in one graph; rows, starts, positions and slots change between the replays."""
+    t, hq, hk, d, page = 200, 8, 2, 64, 16
+    qkv, starts = torch.zeros((t, (hq + 2 * hk) * d), dtype=torch.bfloat16, device=DEV), ints([0, 0, 0, 0])
+    positions, slots = ints([0] * t), ints([-1] * t)
+    cos_sin = torch.randn((512, d), generator=torch.Generator().manual_seed(1)).to(DEV)
+    k_cache, v_cache = (torch.zeros((16, hk, page, d), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    k_rows, q_rows = (torch.zeros((t, h * d), dtype=torch.bfloat16, device=DEV) for h in (hk, hq))
+    y = torch.zeros((t, hq * d), dtype=torch.bfloat16, device=DEV)
+
+    def run():
+        B.rope_cache_write(qkv, cos_sin, positions, slots, k_cache, v_cache, q_out=q_rows, k_out=k_rows)
+        B.attention_prompt(q_rows.view(t, hq, d), k_rows.view(t, hk, d), qkv[:, (hq + hk) * d:].unflatten(1, (hk, d)), starts, out=y)
+
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for seed, cuts in enumerate(([0, 200, 200, 200], [0, 64, 65, 130], [0, 0, 0, 199], [10, 80, 90, 200])):
+        qkv.copy_(randn(seed, *qkv.shape))
+        starts.copy_(ints(cuts))
+        positions.copy_(torch.arange(t) + 7 * seed)
+        slots.copy_(torch.randperm(256, generator=torch.Generator().manual_seed(seed))[:t])
+        results = []
+        for call in (graph.replay, run):
+            for x in (k_cache, v_cache, y):
+                x.zero_()
+            call()
+            torch.cuda.synchronize()
+            results.append([x.clone() for x in (k_cache, v_cache, y)])
+        assert all(torch.equal(a, b) for a, b in zip(*results))
+        assert results[0][2][cuts[0]:cuts[-1]].any() and not results[0][2][:cuts[0]].any() and not results[0][2][cuts[-1]:].any()
