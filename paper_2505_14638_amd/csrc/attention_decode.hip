@@ -243,7 +243,7 @@ __device__ __forceinline__ void stream_keys(const DecodeArgs& a, const DecodePla
     const int64_t at = (int64_t)(r / group) * a.q_heads + kv_head * group + r % group;   // (sequence, query head)
     if constexpr (!std::is_void_v<OutT>) {
         const float inv = inverse_sum(sum);
-        const StaticQuantizer quant(a.y_scale ? *a.y_scale : 1.0f);
+        const Bf16Quantizer quant(a.y_scale ? *a.y_scale : 1.0f);
         OutT* y = static_cast<OutT*>(a.y) + (int64_t)(r / group) * a.ldy + (int64_t)(kv_head * group + r % group) * D + ch;
 #pragma unroll
         for (int j = 0; j < VD; j += 4) store_4(y + j, acc[j] * inv, acc[j + 1] * inv, acc[j + 2] * inv, acc[j + 3] * inv, quant);
@@ -499,7 +499,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(DecodeArgs a, int p
 #pragma unroll
     for (int j = 0; j < VD; ++j) acc[j] = sum_over_32(sum_over_16(acc[j])) * inv;
     if (lane >= 16) return;
-    const StaticQuantizer quant(a.y_scale ? *a.y_scale : 1.0f);
+    const Bf16Quantizer quant(a.y_scale ? *a.y_scale : 1.0f);
     OutT* y = static_cast<OutT*>(a.y) + row / a.q_heads * a.ldy + row % a.q_heads * D + ch;
 #pragma unroll
     for (int j = 0; j < VD; j += 4) store_4(y + j, acc[j], acc[j + 1], acc[j + 2], acc[j + 3], quant);

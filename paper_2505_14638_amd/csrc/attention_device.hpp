@@ -64,16 +64,41 @@ constexpr float RISE = 8.0f;
 // 1 / sum of a finished row; a row that saw nothing (sum 0) gives zeros.
 __device__ __forceinline__ float inverse_sum(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 
+// h / s rounded to float32 and then to E4M3, as the activation quantization does it, for values h that are bf16: two instructions a quotient.
+// high + low is 1 / s up to 2^-45 of it, so h * low + h * high rounds as h / s does, unless h / s lies within 2^-45 of the middle of two
+// neighbouring floats.  That changes the byte only if one of the two is a border of E4M3, of five significant bits: then h 2^j = S (K 2^20 +-
+// 1) + e with h of 8 bits, S (the scale's) of 24, K = 16 .. 31 and |e| < 32, so S = A 2^20 + f with A = 8 .. 16 and |f| <= 32, and f K = -+A
+// modulo 2^20: only K = A = 16 with S = 2^24 - 1, a scale that takes the division.  low has the sign of s and is never zero: zeros keep
+// their sign and infinities meet no zero.  Thirteen prompts of 1 .. 1531 tokens, 32 heads: 135 -> 128 us.
+struct Bf16Quantizer {
+    float s, high, low;
+    bool plain;                                                  // wave-uniform
+    __device__ __forceinline__ explicit Bf16Quantizer(float scale) : s(scale), plain(plain_divisor(scale) && (~__float_as_uint(scale) & 0x7FFFFF) != 0) {
+        high = 1.0f / scale;
+        float rest = fmaf(-scale, high, 1.0f);                   // exact
+        if (rest < 0.0f) {                                       // 1 / s rounded away from zero: the float before it
+            high = __uint_as_float(__float_as_uint(high) - 1);
+            rest = fmaf(-scale, high, 1.0f);
+        }
+        low = fmaxf(rest, 0x1p-60f) * high;
+    }
+    __device__ __forceinline__ float quotient(float h) const { return fmaf(h, high, h * low); }
+    __device__ __forceinline__ uint32_t four(float a, float b, float c, float d) const {
+        if (plain) return cvt2(quotient(c), quotient(d), cvt2(quotient(a), quotient(b), 0u, false), true);
+        return cvt2(c / s, d / s, cvt2(a / s, b / s, 0u, false), true);
+    }
+};
+
 // Four bf16 (two in each word) to four E4M3 bytes, those that the activation quantization makes of them.
-__device__ __forceinline__ uint32_t quant_bf16(uint32_t lo, uint32_t hi, const StaticQuantizer& q) {
+__device__ __forceinline__ uint32_t quant_bf16(uint32_t lo, uint32_t hi, const Bf16Quantizer& q) {
     return q.four(__uint_as_float(lo << 16), __uint_as_float(lo & 0xFFFF0000u), __uint_as_float(hi << 16), __uint_as_float(hi & 0xFFFF0000u));
 }
 
 // Four finished channels of a row, to 8 bytes of bf16 or to 4 E4M3 bytes of those bf16 values.
-__device__ __forceinline__ void store_4(uint16_t* p, float a, float b, float c, float d, const StaticQuantizer&) {
+__device__ __forceinline__ void store_4(uint16_t* p, float a, float b, float c, float d, const Bf16Quantizer&) {
     *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
 }
-__device__ __forceinline__ void store_4(uint8_t* p, float a, float b, float c, float d, const StaticQuantizer& q) {
+__device__ __forceinline__ void store_4(uint8_t* p, float a, float b, float c, float d, const Bf16Quantizer& q) {
     *reinterpret_cast<uint32_t*>(p) = quant_bf16(pack_bf16(a, b), pack_bf16(c, d), q);
 }
 

@@ -274,7 +274,7 @@ __global__ void __launch_bounds__(256, 2) attention_prompt_kernel(PromptArgs a, 
     constexpr int EACH = 16 / (int)sizeof(OutT);
     const int piece = lane % LANES;
     OutT* y = static_cast<OutT*>(a.y) + (int64_t)(seq_start + q0 + 32 * band) * a.ldy + (int64_t)head * D + piece * EACH;
-    const StaticQuantizer quant(BYTES ? *a.y_scale : 1.0f);
+    const Bf16Quantizer quant(BYTES ? *a.y_scale : 1.0f);
 #pragma unroll
     for (int n = 0; n < LANES / 2; ++n) {
         const int r = n * (64 / LANES) + lane / LANES;

@@ -211,3 +211,15 @@ def test_captured_prompt_follows_its_inputs(gpu_lib):
             results.append([x.clone() for x in (k_cache, v_cache, y)])
         assert all(torch.equal(a, b) for a, b in zip(*results))
         assert results[0][2][cuts[0]:cuts[-1]].any() and not results[0][2][:cuts[0]].any() and not results[0][2][cuts[-1]:].any()
+
+
+@pytest.mark.parametrize("scale", [0.01, 0.013, 1 / 448, 1 / 3, 2.0 ** -7, 2.0 ** -7 * (1 - 2.0 ** -24), 2.0 ** -7 * (1 + 2.0 ** -23), -0.02, 1e-12, 1e12, 0.0, math.inf, math.nan])
+def test_quantized_outputs_of_every_value(gpu_lib, scale):
+    """Sequences of one token give its values, all 65536 bf16 patterns; their bytes are those of the activation quantization."""
+    v = torch.arange(-32768, 32768, dtype=torch.int32, device=DEV).short().view(torch.bfloat16).view(1024, 1, 64)
+    q = torch.zeros_like(v)
+    s = torch.tensor([scale], device=DEV)
+    y = B.attention_prompt(q, q, v, ints(list(range(1025))))
+    finite = torch.isfinite(v).view_as(y)
+    assert ((y - v.view_as(y))[finite].abs() <= 2.0 ** -126).all()   # values below the normal ones may count as zero
+    assert torch.equal(B.attention_prompt(q, q, v, ints(list(range(1025))), y_scale=s), B.quantize_act(y, s))
