@@ -446,6 +446,19 @@ __global__ void __launch_bounds__(256) attention_join_kernel(DecodeArgs a, int p
     const int lane = threadIdx.x & 63;
     const int64_t total = (int64_t)a.n_seqs * a.q_heads, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= total) return;
+    const int ch = lane % 16 * VD;
+    const float* from = a.partial + row * D + ch;
+    float4 x[4][VD / 4];
+    auto load = [&](int base) {                                  // parts base + {0 .. 15}; one that nothing is in may hold anything
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int p = base + 4 * i + lane / 16;
+            if (p < parts)
+#pragma unroll
+                for (int j = 0; j < VD / 4; ++j) x[i][j] = *reinterpret_cast<const float4*>(from + p * total * D + 4 * j);
+        }
+    };
+    load(0);                                                     // before their weights are known: one wait instead of two
     const float2* ml = reinterpret_cast<const float2*>(a.partial + parts * total * D) + row;
     float2 t[2];
 #pragma unroll
@@ -463,35 +476,22 @@ __global__ void __launch_bounds__(256) attention_join_kernel(DecodeArgs a, int p
 #pragma unroll
     for (int d = 1; d < 16; d <<= 1) sum += __shfl_xor(sum, d);
     sum = sum_over_32(sum_over_16(sum));
-    const int ch = lane % 16 * VD;
     float acc[VD];
 #pragma unroll
     for (int j = 0; j < VD; ++j) acc[j] = 0.0f;
-    const float* from = a.partial + row * D + ch;
     for (int base = 0; base < parts; base += 16) {
-        float4 x[4][VD / 4];
-        float w[4];
+        if (base > 0) load(base);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (base + 4 * i >= parts) {
-                w[i] = 0.0f;
-                continue;
-            }
-            const int p = base + 4 * i + lane / 16;
-            w[i] = __shfl(base < 64 ? f[0] : f[1], p & 63);      // (no part, or one that is empty: 0)
-            if (w[i] == 0.0f) continue;
-#pragma unroll
-            for (int j = 0; j < VD / 4; ++j) x[i][j] = *reinterpret_cast<const float4*>(from + p * total * D + 4 * j);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (w[i] == 0.0f) continue;
+            if (base + 4 * i >= parts) break;
+            const float w = __shfl(base < 64 ? f[0] : f[1], (base + 4 * i + lane / 16) & 63);
+            if (w == 0.0f) continue;                             // no part, or one that is empty
 #pragma unroll
             for (int j = 0; j < VD / 4; ++j) {
-                acc[4 * j] = fmaf(x[i][j].x, w[i], acc[4 * j]);
-                acc[4 * j + 1] = fmaf(x[i][j].y, w[i], acc[4 * j + 1]);
-                acc[4 * j + 2] = fmaf(x[i][j].z, w[i], acc[4 * j + 2]);
-                acc[4 * j + 3] = fmaf(x[i][j].w, w[i], acc[4 * j + 3]);
+                acc[4 * j] = fmaf(x[i][j].x, w, acc[4 * j]);
+                acc[4 * j + 1] = fmaf(x[i][j].y, w, acc[4 * j + 1]);
+                acc[4 * j + 2] = fmaf(x[i][j].z, w, acc[4 * j + 2]);
+                acc[4 * j + 3] = fmaf(x[i][j].w, w, acc[4 * j + 3]);
             }
         }
     }

@@ -9,17 +9,19 @@ namespace w4a8 {
 namespace {
 
 constexpr int XCDS_A = 8;
-// Sum over the wavefront.
-__device__ __forceinline__ int wave_sum(int x) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xF, 0xF, true);      // lanes 1, 0, 3, 2
-    x += __builtin_amdgcn_update_dpp(0, x, 0x4E, 0xF, 0xF, true);      // lanes 2, 3, 0, 1
-    x += __builtin_amdgcn_update_dpp(0, x, 0x141, 0xF, 0xF, true);     // mirrored in eight
-    x += __builtin_amdgcn_update_dpp(0, x, 0x140, 0xF, 0xF, true);     // mirrored in sixteen
+// Sum or maximum over the wavefront.
+template <bool MAX> __device__ __forceinline__ int wave_reduce(int x) {
+    auto join = [](int a, int b) { return MAX ? max(a, b) : a + b; };
+    x = join(x, __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xF, 0xF, true));    // lanes 1, 0, 3, 2
+    x = join(x, __builtin_amdgcn_update_dpp(0, x, 0x4E, 0xF, 0xF, true));    // lanes 2, 3, 0, 1
+    x = join(x, __builtin_amdgcn_update_dpp(0, x, 0x141, 0xF, 0xF, true));   // mirrored in eight
+    x = join(x, __builtin_amdgcn_update_dpp(0, x, 0x140, 0xF, 0xF, true));   // mirrored in sixteen
     auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    x = (int)(p[0] + p[1]);
+    x = join((int)p[0], (int)p[1]);
     p = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    return uniform((int)(p[0] + p[1]));
+    return uniform(join((int)p[0], (int)p[1]));
 }
+__device__ __forceinline__ int wave_sum(int x) { return wave_reduce<false>(x); }
 
 // Unit t (0 .. tiles - 1) of the packed batch: a sequence and a tile of its rows; false behind the last.  Causal tiles cost what their place
 // in the sequence says, so up to 64 sequences (a lane each) give their tiles in falling order of it, all the sequences' together: the
@@ -37,10 +39,14 @@ __device__ __forceinline__ bool find_tile(const int32_t* starts, int n_seqs, int
         }
         const int mine = (n + BM - 1) / BM;
         int first;                                               // the lane of the sequence
-        if (n_seqs <= 64) {
+        if (n_seqs == 1) {
+            first = 0;
+            tile = __builtin_amdgcn_readlane(mine, 0) - 1 - t;
+            if (tile < 0) return false;
+        } else if (n_seqs <= 64) {
             if (t >= wave_sum(mine)) return false;
             // the place: the lowest that at most t tiles lie behind
-            int low = 0, high = (int)((T + BM - 1) / BM);
+            int low = 0, high = wave_reduce<true>(mine) - 1;
             while (low < high) {
                 const int middle = (low + high) >> 1;
                 if (wave_sum(max(0, mine - 1 - middle)) <= t) high = middle;
