@@ -438,13 +438,14 @@ __global__ void __launch_bounds__(64 * WAVES_D, 2) attention_shared_kernel(Decod
     else stream_keys<D, E4M3, WAVES_D, void>(a, plan, blockIdx.x - prefix_blocks, own_units, lds);
 }
 
-// Joins the parts of a row, a wavefront per row: every lane weighs a part (or two), then sixteen lanes read a part's channels, four parts
-// at a time.
-template <int D, typename OutT>
+// Joins the parts of a row, a wavefront per row, or four of them where a row has more parts than one reads at once (16): every lane weighs a
+// part (or two), then sixteen lanes read a part's channels.
+constexpr int PARTS_AT_ONCE = 16;
+template <int D, int WAVES, typename OutT>
 __global__ void __launch_bounds__(256) attention_join_kernel(DecodeArgs a, int parts) {
     constexpr int VD = D / 16;
-    const int lane = threadIdx.x & 63;
-    const int64_t total = (int64_t)a.n_seqs * a.q_heads, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), first = wave % WAVES * PARTS_AT_ONCE;
+    const int64_t total = (int64_t)a.n_seqs * a.q_heads, row = (int64_t)blockIdx.x * (4 / WAVES) + wave / WAVES;
     if (row >= total) return;
     const int ch = lane % 16 * VD;
     const float* from = a.partial + row * D + ch;
@@ -458,7 +459,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(DecodeArgs a, int p
                 for (int j = 0; j < VD / 4; ++j) x[i][j] = *reinterpret_cast<const float4*>(from + p * total * D + 4 * j);
         }
     };
-    load(0);                                                     // before their weights are known: one wait instead of two
+    load(first);                                                 // before their weights are known: one wait instead of two
     const float2* ml = reinterpret_cast<const float2*>(a.partial + parts * total * D) + row;
     float2 t[2];
 #pragma unroll
@@ -479,8 +480,8 @@ __global__ void __launch_bounds__(256) attention_join_kernel(DecodeArgs a, int p
     float acc[VD];
 #pragma unroll
     for (int j = 0; j < VD; ++j) acc[j] = 0.0f;
-    for (int base = 0; base < parts; base += 16) {
-        if (base > 0) load(base);
+    for (int base = first; base < parts; base += WAVES * PARTS_AT_ONCE) {
+        if (base != first) load(base);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (base + 4 * i >= parts) break;
@@ -498,11 +499,35 @@ __global__ void __launch_bounds__(256) attention_join_kernel(DecodeArgs a, int p
     const float inv = inverse_sum(sum);
 #pragma unroll
     for (int j = 0; j < VD; ++j) acc[j] = sum_over_32(sum_over_16(acc[j])) * inv;
+    if constexpr (WAVES > 1) {
+        __shared__ float4 others[WAVES - 1][VD / 4][16];
+        if (wave > 0 && lane < 16)
+#pragma unroll
+            for (int j = 0; j < VD; j += 4) others[wave - 1][j / 4][lane] = make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
+        __syncthreads();
+        if (wave > 0 || lane >= 16) return;
+#pragma unroll
+        for (int w = 0; w < WAVES - 1; ++w)
+#pragma unroll
+            for (int j = 0; j < VD; j += 4) {
+                const float4 y = others[w][j / 4][lane];
+                acc[j] += y.x;
+                acc[j + 1] += y.y;
+                acc[j + 2] += y.z;
+                acc[j + 3] += y.w;
+            }
+    }
     if (lane >= 16) return;
     const Bf16Quantizer quant(a.y_scale ? *a.y_scale : 1.0f);
     OutT* y = static_cast<OutT*>(a.y) + row / a.q_heads * a.ldy + row % a.q_heads * D + ch;
 #pragma unroll
     for (int j = 0; j < VD; j += 4) store_4(y + j, acc[j], acc[j + 1], acc[j + 2], acc[j + 3], quant);
+}
+
+template <int D, int WAVES> void launch_join(const DecodeArgs& a, int parts, hipStream_t st) {
+    const dim3 grid((unsigned)(((int64_t)a.n_seqs * a.q_heads * WAVES + 3) / 4)), block(256);
+    if (a.y_scale) hipLaunchKernelGGL((attention_join_kernel<D, WAVES, uint8_t>), grid, block, 0, st, a, parts);
+    else hipLaunchKernelGGL((attention_join_kernel<D, WAVES, uint16_t>), grid, block, 0, st, a, parts);
 }
 
 template <int D, bool E4M3, int W, typename OutT>
@@ -531,9 +556,8 @@ void launch_typed(const DecodeArgs& a, const DecodePlan& p, hipStream_t st) {
         const int blocks = (shared + 7) / 8 * 8;
         hipLaunchKernelGGL((attention_shared_kernel<D, E4M3>), dim3((unsigned)(blocks + own)), dim3(64 * WAVES_D), 0, st, a, p, own, row_tiles, shared, blocks);
     }
-    const dim3 grid((unsigned)(((int64_t)a.n_seqs * a.q_heads + 3) / 4));
-    if (a.y_scale) hipLaunchKernelGGL((attention_join_kernel<D, uint8_t>), grid, dim3(256), 0, st, a, p.parts);
-    else hipLaunchKernelGGL((attention_join_kernel<D, uint16_t>), grid, dim3(256), 0, st, a, p.parts);
+    if (p.parts > PARTS_AT_ONCE) launch_join<D, 4>(a, p.parts, st);
+    else launch_join<D, 1>(a, p.parts, st);
 }
 
 }  // namespace
