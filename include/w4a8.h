@@ -391,7 +391,8 @@ int w4a8_linear_silu_mul_fp8_out(const uint8_t* x8_dev, int64_t M, int64_t K, in
  *               Elements bf16, or E4M3 bytes that stand for byte * kv_scales_dev[0] (keys), byte * kv_scales_dev[1] (values): static
  *               per-tensor scales, as for activations (Eq. 13).  kv_scales_dev is read for E4M3 only
  *   tables_dev  int32 page numbers: position j of a sequence is token j % P of page table[j / P].  Sequences may list the same page
- *   rows        row strides (ld*) in elements, below 2^20; rows are 16-byte aligned (pointer and stride)
+ *   rows        row strides (ld*) in elements, below 2^20; rows are 16-byte aligned (pointer and stride).  Outputs overlap no input, save where it is
+ *               said
  *
  * w4a8_rope_cache_write: for each token t of a QKV layer's output, qkv_dev [T, (H + 2 HK) * D] (query heads, key heads, value heads),
  *   turns every query and key head by the angles of row positions_dev[t] of cos_sin_dev (float32 [table_rows, D]: D/2 cosines, then

@@ -11,11 +11,15 @@ using namespace w4a8;
 namespace w4a8 {
 
 // A workgroup on the sequences' own tokens reads one range of keys for up to 16 rows.  Few sequences need enough ranges to give every
-// compute unit two workgroups (FILL), of SHORT keys at least; more of them cost more by their starts and partial results than they even out (64
-// sequences of 200 .. 8192 tokens, 64 heads, E4M3: 131 us with one range, 152 with up to eight).
-// Up to ONE_GO tokens one workgroup of eight wavefronts takes them all, however few there are of those: that saves the second launch.
-// On the prefix up to 16 rows go the same way.  More rows walk tiles of 64 keys that 128 rows share; there a range costs its tiles, and
-// every part of a row 4 (D + 2) bytes written and read again, about 4.5 TB/s.
+// compute unit two workgroups (FILL), of SHORT keys at least; more of them cost more by their starts and partial results than they even out.  Figures
+// in us, 32 query and 8 key heads, bf16:  3 sequences of 500 .. 16000 (E4M3) 21.0, with FILL 256 23.7; 16 of 4000 52.0, with 1024 53.3; one of
+// 1000 7.5, with SHORT 256 9.0; 64 of 200 .. 8192, 64 heads, E4M3, 131 with one range, 152 with up to eight.
+// Up to ONE_GO tokens one workgroup of eight wavefronts takes them all, however few there are of those: that saves the second launch, 3 us of the
+// host's time beside the device's: 20 sequences of 500 10.6, in two launches 14.7; one of 200 6.0 and 7.4, of 500 8.6 and 7.5; one of 1000
+// would take 13.4 and 7.4.
+// On the prefix up to 16 rows go the same way (one sequence of 500 behind 4000: 10.2, as tiles 11.3).  More rows walk tiles of 64 keys that 128
+// rows share (16 sequences: 15.8, by sixteens 23.7); there a range costs its tiles, and every part of a row 4 (D + 2) bytes written and read
+// again, about 4.5 TB/s.
 DecodePlan decode_plan(int64_t n_seqs, int q_heads, int kv_heads, int head_dim, int64_t own_capacity, int64_t prefix_len) {
     constexpr int64_t FILL = 512, SHORT = 128, MOST = 64, CUS = 256, ONE_GO = 512;
     const int64_t group = q_heads / kv_heads, rows = n_seqs * group, own_units = n_seqs * kv_heads * ((group + 15) / 16);

@@ -105,7 +105,8 @@ __global__ void __launch_bounds__(256) rope_cache_write_kernel(RopeCacheArgs a, 
     }
 }
 
-// One workgroup copies up to 32 KiB of one page of one plane, eight 16-byte pieces per thread under way at once.
+// One workgroup copies up to 32 KiB of one page of one plane, eight 16-byte pieces per thread under way at once.  Memory bounds it: 400 pages of 64
+// planes, 32 KB each, 1.68 GB read and written: 318 us, 5.3 TB/s, where a large copy by the runtime reaches 4.8; 16 pages: 11.6 us.
 constexpr int COPY_PIECES = 8, COPY_BYTES = 256 * 16 * COPY_PIECES;
 __global__ void __launch_bounds__(256) cache_copy_pages_kernel(uint8_t* cache, int64_t plane_stride, int64_t n_pages, int64_t page_stride,
                                                                int64_t page_bytes, const int32_t* src, const int32_t* dst, int64_t n_copies,
