@@ -19,7 +19,8 @@ namespace w4a8 {
 // would take 13.4 and 7.4.
 // On the prefix up to 16 rows go the same way (one sequence of 500 behind 4000: 10.2, as tiles 11.3).  More rows walk tiles of 64 keys that 128
 // rows share (16 sequences: 15.8, by sixteens 23.7); there a range costs its tiles, and every part of a row 4 (D + 2) bytes written and read
-// again, about 4.5 TB/s.
+// again, together about 3 TB/s; the figures of that sum are measured ones (32 sequences of 1 .. 512 behind 4096: 20.5, 64 of 100 .. 1000 behind 2000: 40.8; with
+// 1.6 us a tile and 4.5 TB/s 22.3 and 45.9, with 2 TB/s 20.6 and 41.3).
 DecodePlan decode_plan(int64_t n_seqs, int q_heads, int kv_heads, int head_dim, int64_t own_capacity, int64_t prefix_len) {
     constexpr int64_t FILL = 512, SHORT = 128, MOST = 64, CUS = 256, ONE_GO = 512;
     const int64_t group = q_heads / kv_heads, rows = n_seqs * group, own_units = n_seqs * kv_heads * ((group + 15) / 16);
@@ -37,10 +38,10 @@ DecodePlan decode_plan(int64_t n_seqs, int q_heads, int kv_heads, int head_dim, 
         p.prefix_splits = splits(kv_heads, prefix_len);
     } else {
         const int64_t units = kv_heads * ((rows + p.prefix_rows - 1) / p.prefix_rows), tiles = (prefix_len + 63) / 64;
-        const double part_us = (double)n_seqs * q_heads * 8 * (head_dim + 2) / 4.5e6;
+        const double part_us = (double)n_seqs * q_heads * 8 * (head_dim + 2) / 3.0e6;
         double best = 0;
         for (int64_t s = 1; s <= MOST && s <= tiles; ++s) {
-            const double us = (double)((units * s + CUS - 1) / CUS) * (1.6 * (double)((tiles + s - 1) / s) + 4) + (double)s * part_us;
+            const double us = (double)((units * s + CUS - 1) / CUS) * (1.4 * (double)((tiles + s - 1) / s) + 4) + (double)s * part_us;
             if (s == 1 || us < best) best = us, p.prefix_splits = (int)s;
         }
     }

@@ -444,10 +444,11 @@ __global__ void __launch_bounds__(64 * WAVES_D, 2) attention_shared_kernel(Decod
     else stream_keys<D, E4M3, WAVES_D, void>(a, plan, blockIdx.x - prefix_blocks, own_units, lds);
 }
 
-// Joins the parts of a row, a wavefront per row, or four of them where a row has more parts than one reads at once (16): every lane weighs a
-// part (or two), then sixteen lanes read a part's channels.  Latency bounds it: one sequence of 16000 tokens in 64 parts, stream and join, 17.1 us, 20.4
-// with one wavefront a row.
-constexpr int PARTS_AT_ONCE = 16;
+// Joins the parts of a row, a wavefront per row, or four of them where a row has more parts than one reads at once and the rows are no more than
+// the compute units: every lane weighs a part (or two), then sixteen lanes read a part's channels.  Latency bounds it: one sequence of 16000 tokens
+// in 64 parts, stream and join, 17.0 us, 20.4 with one wavefront a row; 32 sequences behind 4096 tokens (1024 rows, 17 parts) the other way
+// round, 21.4 and 16.7.
+constexpr int PARTS_AT_ONCE = 16, FEW_ROWS = 256;
 template <int D, int WAVES, typename OutT>
 __global__ void __launch_bounds__(256) attention_join_kernel(DecodeArgs a, int parts) {
     constexpr int VD = D / 16;
@@ -563,7 +564,7 @@ void launch_typed(const DecodeArgs& a, const DecodePlan& p, hipStream_t st) {
         const int blocks = (shared + 7) / 8 * 8;
         hipLaunchKernelGGL((attention_shared_kernel<D, E4M3>), dim3((unsigned)(blocks + own)), dim3(64 * WAVES_D), 0, st, a, p, own, row_tiles, shared, blocks);
     }
-    if (p.parts > PARTS_AT_ONCE) launch_join<D, 4>(a, p.parts, st);
+    if (p.parts > PARTS_AT_ONCE && (int64_t)a.n_seqs * a.q_heads <= FEW_ROWS) launch_join<D, 4>(a, p.parts, st);
     else launch_join<D, 1>(a, p.parts, st);
 }
 

@@ -223,3 +223,18 @@ def test_quantized_outputs_of_every_value(gpu_lib, scale):
     finite = torch.isfinite(v).view_as(y)
     assert ((y - v.view_as(y))[finite].abs() <= 2.0 ** -126).all()   # values below the normal ones may count as zero
     assert torch.equal(B.attention_prompt(q, q, v, ints(list(range(1025))), y_scale=s), B.quantize_act(y, s))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("lengths,prefix,hq,hk,d", [([5000], 0, 4, 2, 128), ([8300, 3], 0, 6, 1, 64), ([8192], 8192, 4, 1, 64), ([40] * 30, 3000, 8, 1, 128), ([300] * 40, 2500, 16, 2, 64)])
+def test_decode_in_many_parts(gpu_lib, lengths, prefix, hq, hk, d, cache):
+    """More partial results than a wavefront joins at once, up to 128, with few rows and with many."""
+    k, v, scales, tables, prefix_pages = paged(prefix + 1, lengths, prefix, hk, d, 16, cache)
+    q = randn(7, len(lengths), hq, d).bfloat16()
+    args = dict(prefix_pages=ints(prefix_pages) if prefix else None, prefix_length=prefix, kv_scales=scales)
+    y = B.attention_decode(q, k, v, ints(tables), ints(lengths), **args)
+    k_scale, v_scale = (None, None) if scales is None else scales.tolist()
+    out, size = R.decode(q, R.cache_values(k, k_scale), R.cache_values(v, v_scale), tables, lengths, d, prefix_pages, prefix)
+    assert R.worst(y, out, size) <= 1.0
+    y_scale = torch.tensor([0.013], device=DEV)
+    assert torch.equal(B.attention_decode(q, k, v, ints(tables), ints(lengths), y_scale=y_scale, **args), B.quantize_act(y, y_scale))
