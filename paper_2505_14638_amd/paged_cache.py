@@ -117,11 +117,11 @@ class PagedCache:
                 common += 1
         width = max([len(p) - common for p in lists] + [1])
         rows = [p[common:] + [0] * (width - len(p) + common) for p in lists]
-        return (self._ints(rows), self._ints([n - common * self.page_size for n in lengths]), self._ints(lists[0][:common]) if common else None,
+        return (self._ints(rows).reshape(len(seqs), width), self._ints([n - common * self.page_size for n in lengths]), self._ints(lists[0][:common]) if common else None,
                 common * self.page_size)
 
     def compact(self) -> int:
-        """Moves pages so that the used ones are the lowest; returns how many those are.  Tables from before are void."""
+        """Moves pages so that the used ones are the lowest; returns how many those are.  Tables and slots from before are void."""
         used = sum(u > 0 for u in self._uses)
         src = [p for p in range(used, len(self._uses)) if self._uses[p] > 0]
         dst = [p for p in range(used) if self._uses[p] == 0]

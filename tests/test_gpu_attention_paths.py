@@ -238,3 +238,19 @@ def test_decode_in_many_parts(gpu_lib, lengths, prefix, hq, hk, d, cache):
     assert R.worst(y, out, size) <= 1.0
     y_scale = torch.tensor([0.013], device=DEV)
     assert torch.equal(B.attention_decode(q, k, v, ints(tables), ints(lengths), y_scale=y_scale, **args), B.quantize_act(y, y_scale))
+
+
+def test_calls_without_tokens(gpu_lib):
+    hq, hk, d = 4, 2, 64
+    q, k, v = prompt_inputs(1, 0, hq, hk, d)
+    assert B.attention_prompt(q, k, v, ints([0])).shape == (0, hq * d) and B.attention_prompt(q, k, v, ints([0, 0, 0])).shape == (0, hq * d)
+    q, k, v = prompt_inputs(1, 3, hq, hk, d)
+    assert (B.attention_prompt(q, k, v, ints([2])) == 0).all() and (B.attention_prompt(q, k, v, ints([1, 1, 1])) == 0).all()
+    cache = torch.full((4, hk, 16, d), 5.0, dtype=torch.bfloat16, device=DEV)
+    assert B.attention_decode(q[:0], cache, cache, ints([]).view(0, 1), ints([])).shape == (0, hq * d)
+    assert (B.attention_decode(q, cache, cache, ints([]).view(3, 0), ints([7, 0, -1])) == 0).all()
+    cos_sin = torch.ones((8, d), device=DEV)
+    assert B.rope_cache_write(randn(1, 0, (hq + 2 * hk) * d).bfloat16(), cos_sin, ints([]), ints([]), cache, cache).shape == (0, hq * d)
+    B.cache_copy_pages(cache.unsqueeze(0), ints([]), ints([]))
+    torch.cuda.synchronize()
+    assert (cache == 5).all()

@@ -109,3 +109,11 @@ def test_refusals():
     with pytest.raises(KeyError):
         cache.grow([seq + 1], [1])
     assert cache.length(seq) == 0 and cache.free_pages == 4
+
+
+def test_an_empty_batch():
+    cache = PagedCache(1, 4, 1, 64, device="cpu")
+    positions, slots = cache.grow([], [])
+    tables, lengths, prefix_pages, prefix_length = cache.tables([])
+    assert positions.numel() == slots.numel() == lengths.numel() == prefix_length == 0 and prefix_pages is None and tuple(tables.shape) == (0, 1)
+    assert cache.compact() == 0 and cache.free_pages == 4
