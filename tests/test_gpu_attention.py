@@ -174,7 +174,7 @@ def test_decode_lengths_and_pages_out_of_range(gpu_lib):
 @pytest.mark.parametrize("cache", ["bf16", "e4m3"])
 @pytest.mark.parametrize("n,d", [(3, 128), (10, 64), (10, 128), (40, 64), (40, 128)])
 def test_prefix_pages_out_of_range(gpu_lib, n, d, cache):
-    """In each kernel that reads a prefix: by 16 rows, by 64 and by 128."""
+    """In each kernel that reads a prefix: by 16 rows and by 128."""
     hq, hk, page, prefix = 8, 2, 16, 500
     k, v, scales, tables, prefix_pages = paged(9, [3] * n, prefix, hk, d, page, cache, fill=NAN if cache == "bf16" else None)
     for i, bad in ((0, -1), (5, 1 << 30), (6, k.shape[0]), (7, -1), (8, -9), (31, -1)):
