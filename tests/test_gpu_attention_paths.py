@@ -254,3 +254,69 @@ def test_calls_without_tokens(gpu_lib):
     B.cache_copy_pages(cache.unsqueeze(0), ints([]), ints([]))
     torch.cuda.synchronize()
     assert (cache == 5).all()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_a_long_prompt(gpu_lib, causal):
+    """30000 tokens: some rows against 64 bits.  The longest chain of float32 sums is 7500 long: 7500 * 2^-24 < 2^-11 of the result, within the bound's 2^-10."""
+    t, hq, hk, d = 30000, 2, 1, 64
+    q, k, v = prompt_inputs(12, t, hq, hk, d)
+    y = B.attention_prompt(q, k, v, ints([0, t]), causal=causal).view(t, hq, d)
+    kk, vv = R.heads(k, d)[:, 0], R.heads(v, d)[:, 0]
+    rows = [0, 1, 63, 64, 127, 128, 4095, 14999, 15000, 29951, 29952, 29999]
+    hidden = torch.arange(t)[None] > torch.tensor(rows)[:, None] if causal else None
+    for h in range(hq):
+        out, size = R.attend(R.heads(q, d)[rows, h], kk, vv, d ** -0.5, hidden)
+        assert R.worst(y[rows, h], out, size) <= 1.0
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("length,prefix,n", [(150000, 0, 1), (100, 100001, 20)])
+def test_long_caches(gpu_lib, length, prefix, n, cache):
+    hq, hk, d, page = 2, 1, 64, 128
+    k, v, scales, tables, prefix_pages = paged(3, [length] * n, prefix, hk, d, page, cache)
+    q = randn(9, n, hq, d).bfloat16()
+    y = B.attention_decode(q, k, v, ints(tables), ints([length] * n), ints(prefix_pages) if prefix else None, prefix, scales)
+    k_scale, v_scale = (None, None) if scales is None else scales.tolist()
+    out, size = R.decode(q[-1:], R.cache_values(k, k_scale), R.cache_values(v, v_scale), tables[-1:], [length], d, prefix_pages, prefix)
+    assert R.worst(y[-1:], out, size) <= 1.0
+
+
+@pytest.mark.parametrize("n", [2, 20])
+@pytest.mark.parametrize("cache,d", [("bf16", 64), ("bf16", 128), ("e4m3", 64), ("e4m3", 128)])
+def test_decode_with_values_that_are_no_numbers(gpu_lib, cache, d, n):
+    """NaN behind the lengths and the prefix's end changes nothing; seen, in one channel of one key head, it reaches that channel of the rows that see it."""
+    hq, hk, page, prefix = 8, 2, 32, 150                         # the prefix ends inside a page, the lengths too
+    lengths = [45 + i for i in range(n)]
+    k, v, scales, tables, prefix_pages = paged(5, lengths, prefix, hk, d, page, cache)
+    q = randn(9, n, hq, d).bfloat16()
+    none = math.nan if cache == "bf16" else 0x7F
+
+    def run(k, v):
+        y = B.attention_decode(q, k, v, ints(tables), ints(lengths), ints(prefix_pages), prefix, scales)
+        return y.view(n, hk, hq // hk, d)
+
+    y = run(k, v)
+    k2, v2 = k.clone(), v.clone()
+    for x in (k2, v2):
+        x[prefix_pages[-1], :, prefix % page:] = none
+        for b, length in enumerate(lengths):
+            if length % page:
+                x[tables[b][length // page], :, length % page:] = none
+        x[[p for p in range(len(x)) if p not in prefix_pages and not any(p in t[:-(-m // page)] for t, m in zip(tables, lengths))]] = none
+    assert torch.equal(run(k2, v2), y) and not torch.isnan(y).any()
+    v3 = v2.clone()
+    v3[tables[1][1], 1, 3, 7] = none                             # token 35 of sequence 1
+    want = y.clone()
+    want[1, 1, :, 7] = math.nan
+    assert torch.equal(run(k2, v3).nan_to_num(1e30), want.nan_to_num(1e30))
+    v3 = v2.clone()
+    v3[prefix_pages[4], 0, 21, 3] = none                         # token 149 of the prefix, its last one
+    want = y.clone()
+    want[:, 0, :, 3] = math.nan
+    assert torch.equal(run(k2, v3).nan_to_num(1e30), want.nan_to_num(1e30))
+    k3 = k2.clone()
+    k3[prefix_pages[0], 1, 0, 0] = none                          # a key: all that its head's rows become
+    want = y.clone()
+    want[:, 1] = math.nan
+    assert torch.equal(run(k3, v2).nan_to_num(1e30), want.nan_to_num(1e30))
