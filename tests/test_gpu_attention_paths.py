@@ -320,3 +320,29 @@ def test_decode_with_values_that_are_no_numbers(gpu_lib, cache, d, n):
     want = y.clone()
     want[:, 1] = math.nan
     assert torch.equal(run(k3, v2).nan_to_num(1e30), want.nan_to_num(1e30))
+
+
+@pytest.mark.parametrize("hk,d", [(1, 64), (1024, 128), (4096, 64)])
+def test_as_many_heads_as_there_may_be(gpu_lib, hk, d):
+    hq = 4096
+    starts = [0, 5, 5, 8]
+    q, k, v = (randn(i, 8, h, d).bfloat16() for i, h in enumerate((hq, hk, hk)))
+    y = B.attention_prompt(q, k, v, ints(starts))
+    out, size = R.prompt(q, k, v, starts, d, True)
+    assert R.worst(y, out, size) <= 1.0
+    lengths = [20, 0, 3]
+    for prefix in (0, 40):
+        kc, vc, _, tables, prefix_pages = paged(prefix, lengths, prefix, hk, d, 16, "bf16", spare=1)
+        y = B.attention_decode(q[:3], kc, vc, ints(tables), ints(lengths), ints(prefix_pages) if prefix else None, prefix)
+        out, size = R.decode(q[:3], R.cache_values(kc), R.cache_values(vc), tables, lengths, d, prefix_pages, prefix)
+        assert R.worst(y, out, size) <= 1.0
+    cos_sin = torch.randn((64, d), generator=torch.Generator().manual_seed(1)).to(DEV)
+    qkv = randn(3, 4, (hq + 2 * hk) * d).bfloat16()
+    turned = B.rope_cache_write(qkv, cos_sin, ints([0, 63, 7, 9]), ints([0, 17, 3, 18]), kc, vc)
+    want = R.rotated(R.heads(qkv, d)[:, :hq], cos_sin, torch.tensor([0, 63, 7, 9]), False).flatten(1)
+    # one rounding to bf16 of two products of up to 6 and 5, and their sum, in float32
+    assert ((turned.cpu().double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -18).all()
+    at = kc[[0, 1, 0, 1], :, [0, 1, 3, 2]], vc[[0, 1, 0, 1], :, [0, 1, 3, 2]]
+    assert torch.equal(at[1].flatten(1), qkv[:, (hq + hk) * d:])
+    want = R.rotated(R.heads(qkv, d)[:, hq:hq + hk], cos_sin, torch.tensor([0, 63, 7, 9]), False)
+    assert ((at[0].cpu().double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -18).all()
