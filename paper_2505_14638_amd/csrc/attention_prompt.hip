@@ -194,7 +194,8 @@ __global__ void __launch_bounds__(256, 2) attention_prompt_kernel(PromptArgs a, 
     }
 
     // A weight of zero takes a key out of the sums, unless its value is no number.  So if an output is none, the rows are walked again with zeros
-    // for such values, and then twice to mark the outputs that see one: all scores are zero there, and every row counts the ones it sees.
+    // for such values, and then twice to mark the outputs that see one: all scores are zero there, and every row counts the ones it sees.  Scores that
+    // are NaN or +infinity are NaN there: such a row's outputs are NaN already, its counts too, and no value changes that.
     uint64_t marked = 0;                                         // outputs of this lane that see +infinity or NaN
     for (;; ++walk) {
     rows.clear();
@@ -212,7 +213,7 @@ __global__ void __launch_bounds__(256, 2) attention_prompt_kernel(PromptArgs a, 
 #pragma unroll
             for (int k = 0; k < KT; ++k)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[k][r] = 0.0f;
+                for (int r = 0; r < 16; ++r) s[k][r] = s[k][r] == NEG_INF ? 0.0f : s[k][r] * 0.0f;
             asm volatile("s_mov_b32 %0, 0" : "=s"(counts));
         }
         const bool masked = key0 + KEYS > len || (CAUSAL && key0 + KEYS - 1 > q0 + 32 * band);
@@ -307,7 +308,7 @@ __global__ void __launch_bounds__(256, 2) attention_prompt_kernel(PromptArgs a, 
         for (int i = 0; i < 16 * D / 32; ++i) {
             const int r = i / EACH * (64 / LANES) + lane / LANES, c = piece * EACH + i % EACH;
             const uint16_t count = lds_read<uint16_t>(slab + r * ROW + (uint32_t)(((c / 8) ^ swizzle<D>(r)) << 4) + c % 8 * 2);
-            if (count == 0 || q0 + 32 * band + r >= len) continue;
+            if (count == 0 || (count & 0x7FFFu) > 0x7F80u || q0 + 32 * band + r >= len) continue;
             OutT* at = y + (int64_t)r * a.ldy + i % EACH;
             if (walk == PLUS) {
                 marked |= (uint64_t)1 << i;

@@ -1,0 +1,73 @@
+"""Attention where scores or values are infinities or NaN, where a row's weights have to come to exactly one, and where rows see nothing, against
+the definition in 64 bits: the softmax of the visible scores, and the sum over the visible values alone."""
+import math
+
+import pytest
+import torch
+
+import attention_reference as R
+from paper_2505_14638_amd import binding as B
+from test_gpu_attention import DEV, ints, paged, prompt_inputs, randn
+
+pytestmark = pytest.mark.gpu
+INF, NAN = math.inf, math.nan
+
+
+def defined(q, k, v, scale, hidden=None):
+    """One query head's rows q [n, D] against keys k, v [m, D], float64: (output, sum of the weights times |v|)."""
+    s = (q @ k.t()) * scale
+    hidden = torch.zeros_like(s, dtype=torch.bool) if hidden is None else hidden
+    w = torch.softmax(torch.where(hidden, -INF, s), dim=1)
+    parts = torch.where(hidden[:, :, None], 0.0, w[:, :, None] * v[None])
+    return parts.sum(dim=1), parts.abs().sum(dim=1)
+
+
+def agrees(y, out, size):
+    """NaN where it is NaN, infinities with their signs, and within the bound of the other tests elsewhere."""
+    y = y.detach().cpu().double()
+    plain = torch.isfinite(out)
+    assert torch.equal(torch.isnan(y), torch.isnan(out))
+    assert torch.equal(y[torch.isinf(out)], out[torch.isinf(out)]) and torch.isfinite(y[plain]).all()
+    assert R.worst(y[plain], out[plain], size[plain]) <= 1.0
+
+
+def check_prompt(q, k, v, causal, heads):
+    """The rows of some heads against the definition; E4M3 output against the quantization of the bf16 one."""
+    t, hq, d = q.shape
+    group = hq // k.shape[1]
+    y = B.attention_prompt(q, k, v, ints([0, t]), causal=causal)
+    hidden = torch.ones((t, t), dtype=torch.bool).triu(1) if causal else None
+    x = [R.heads(a.reshape(t, -1), d) for a in (q, k, v)]
+    for h in heads:
+        agrees(y.view(t, hq, d)[:, h], *defined(x[0][:, h], x[1][:, h // group], x[2][:, h // group], d ** -0.5, hidden))
+    scale = torch.tensor([0.02], device=DEV)
+    assert torch.equal(B.attention_prompt(q, k, v, ints([0, t]), causal=causal, y_scale=scale), B.quantize_act(y, scale))
+
+
+# tiles of 128 rows times heads: few (two wavefronts on the same rows) and many
+SIZES = [(200, 4, 2, 64), (200, 4, 2, 128), (200, 200, 2, 64), (200, 200, 2, 128)]
+
+
+def heads_of(hq):
+    return sorted({0, hq // 2 - 1, hq // 2, hq - 1})
+
+
+def infinite_values(v, at):
+    """Both infinities, apart and together, and NaN among the values of one key head, a channel each."""
+    v = v.clone()
+    v[at, 0, 5], v[at, 0, 6], v[at, 0, 8] = INF, -INF, NAN
+    v[at, 0, 7], v[at + 5, 0, 7] = INF, -INF
+    return v
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("t,hq,hk,d", SIZES)
+def test_scores_that_are_nan_beside_infinite_values(gpu_lib, t, hq, hk, d, causal):
+    """A NaN in a query, or in a key that a row sees, makes all of the row's outputs NaN, whatever its values are."""
+    q, k, v = prompt_inputs(41, t, hq, hk, d)
+    v = infinite_values(v, 30)
+    q[90, :, 3] = NAN
+    check_prompt(q, k, v, causal, heads_of(hq))
+    q[90, :, 3] = 0.5
+    k[70, 0, 3] = NAN
+    check_prompt(q, k, v, causal, heads_of(hq))
