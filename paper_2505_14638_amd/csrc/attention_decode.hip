@@ -309,8 +309,9 @@ __device__ __forceinline__ void walk_prefix(const DecodeArgs& a, const DecodePla
         return p < a.c.n_pages ? p : -1;
     };
     u32x4 held[E4M3 ? 2 * GROUPS * LOADS : 1];                   // E4M3 on its way to LDS
-    // Brings this wavefront's groups of tile t to the buffer (E4M3: to registers).  Rows behind the prefix's end repeat its last one;
-    // a group without tokens becomes zeros: what no row sees must still be numbers.
+    // Brings this wavefront's groups of tile t to the buffer (E4M3: to registers).  What no row sees must still be numbers among the values: rows
+    // behind the prefix's end repeat its last key, and its last value only as E4M3, which has no infinities; bf16 values there are zeros, as
+    // all of a group without tokens.
     auto fetch = [&](int t, int pages, int buffer) {
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) {
@@ -342,7 +343,8 @@ __device__ __forceinline__ void walk_prefix(const DecodeArgs& a, const DecodePla
                     const int r = i * RPC + lane / PIECES;
                     const uint32_t off = (uint32_t)(min(r, last) * ROW + ((lane % PIECES) ^ swizzle<D>(r)) * 16);
                     lds_dma_16(a.k_cache + at, off, to + i * 1024);
-                    lds_dma_16(a.v_cache + at, off, to + TILE + i * 1024);
+                    if (last >= 15) lds_dma_16(a.v_cache + at, off, to + TILE + i * 1024);
+                    else lds_write(to + TILE + i * 1024 + lane * 16, r > last ? u32x4{0, 0, 0, 0} : *reinterpret_cast<const u32x4*>(a.v_cache + at + off));
                 }
             }
         }

@@ -71,3 +71,22 @@ def test_scores_that_are_nan_beside_infinite_values(gpu_lib, t, hq, hk, d, causa
     q[90, :, 3] = 0.5
     k[70, 0, 3] = NAN
     check_prompt(q, k, v, causal, heads_of(hq))
+
+
+@pytest.mark.parametrize("prefix", [145, 150, 159, 160])
+@pytest.mark.parametrize("n", [2, 20])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bad", [INF, -INF, NAN])
+def test_infinite_values_at_the_end_of_a_prefix(gpu_lib, d, n, prefix, bad):
+    """In the last token of a prefix, which may end inside sixteen keys or not: they reach every row that sees it as they are."""
+    hq, hk, page = 8, 2, 32
+    lengths = [45 + i for i in range(n)]
+    k, v, _, tables, prefix_pages = paged(5, lengths, prefix, hk, d, page, "bf16", fill=NAN)
+    q = randn(9, n, hq, d).bfloat16()
+    args = ints(tables), ints(lengths), ints(prefix_pages), prefix
+    want = B.attention_decode(q, k, v, *args).view(n, hk, hq // hk, d)
+    assert torch.isfinite(want).all()
+    v[prefix_pages[-1], 0, (prefix - 1) % page, 3] = bad
+    want[:, 0, :, 3] = bad
+    y = B.attention_decode(q, k, v, *args).view_as(want)
+    assert torch.equal(y.isnan(), want.isnan()) and torch.equal(y.nan_to_num(7.0, INF, -INF), want.nan_to_num(7.0, INF, -INF))
