@@ -169,13 +169,15 @@ __device__ __forceinline__ void stream_keys(const DecodeArgs& a, const DecodePla
             m = m_new;
         }
         const float m_use = m == NEG_INF ? 0.0f : m;
-        float p[8];
+        u32x4 p;                                                 // rounded to bf16, as the product takes them, and so in the sum: they come to one
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            p[i] = exp2_fast(fmaf(s[i / 4][i % 4], score_scale, -m_use));
-            l += p[i];
+        for (int i = 0; i < 4; ++i) {
+            const v4f& x = s[i / 2];
+            const int r = 2 * (i & 1);
+            p[i] = pack_bf16(exp2_fast(fmaf(x[r], score_scale, -m_use)), exp2_fast(fmaf(x[r + 1], score_scale, -m_use)));
+            l = add_pair(p[i], l);
         }
-        const v8bf pf = __builtin_bit_cast(v8bf, u32x4{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])});
+        const v8bf pf = __builtin_bit_cast(v8bf, p);
         // values as bf16 pairs of channels
         uint32_t v[8][VD / 2];
 #pragma unroll

@@ -90,3 +90,26 @@ def test_infinite_values_at_the_end_of_a_prefix(gpu_lib, d, n, prefix, bad):
     want[:, 0, :, 3] = bad
     y = B.attention_decode(q, k, v, *args).view_as(want)
     assert torch.equal(y.isnan(), want.isnan()) and torch.equal(y.nan_to_num(7.0, INF, -INF), want.nan_to_num(7.0, INF, -INF))
+
+
+@pytest.mark.parametrize("spread", [1.0, 3.0, 8.0])
+@pytest.mark.parametrize("d", [64, 128])
+def test_weights_of_a_row_come_to_one(gpu_lib, d, spread):
+    """Where every value is one, so is every output: the sum that divides is that of the weights as they enter the product, rounded to bf16.  Both are
+    float32 sums in chains of less than 512 additions, so at most 2^-14 apart, and what is within 2^-9 of one rounds to it."""
+    hq, hk, t = 8, 2, 700
+    q, k, _ = prompt_inputs(51, t, hq, hk, d)
+    q = (q.float() * spread).bfloat16()
+    one = torch.ones_like(k)
+    for causal in (True, False):
+        assert (B.attention_prompt(q, k, one, ints([0, t]), causal=causal) == 1).all()
+        many = q.repeat(1, 12, 1)
+        assert (B.attention_prompt(many, k, one, ints([0, t]), causal=causal) == 1).all()
+    for cache in ("bf16", "e4m3"):
+        for lengths, prefix in (([300, 1, 17] * 5, 0), ([700], 0), ([60] * 3, 0), ([30] * 100, 0), ([40] * 2, 200), ([40] * 40, 200), ([700] * 256, 0), ([1] * 4, 40000)):
+            k, v, scales, tables, prefix_pages = paged(3, lengths, prefix, hk, d, 16, cache)
+            v.fill_(1.0 if cache == "bf16" else 0x30)            # E4M3: 0.5 times a scale of 2
+            if scales is not None:
+                scales[1] = 2.0
+            y = B.attention_decode(q[:len(lengths)], k, v, ints(tables), ints(lengths), ints(prefix_pages) if prefix else None, prefix, scales)
+            assert (y == 1).all(), (cache, lengths, prefix)
