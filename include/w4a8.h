@@ -402,7 +402,7 @@ int w4a8_linear_silu_mul_fp8_out(const uint8_t* x8_dev, int64_t M, int64_t K, in
  *   values, to slot slots_dev[t] of the cache, page slot / P, token slot % P: rounded to bf16, or nearest_E4M3(x / scale), one float32 division
  *   of the rotated float32 value.  A token whose slot is outside [0, n_pages * P) is padding: nothing is read or written for it.  A position
  *   outside the table gives NaN.  The slots of a call are distinct.  q_out_dev may be qkv_dev itself (ldq = ldqkv), and k_out_dev its key columns.
- *   T <= 2^24.
+ *   T <= 2^24, T * (H + 2 HK) * D / 16 <= 2^32 - 256, table_rows <= 2^30.
  *
  * w4a8_attention_prompt: n_seqs whole prompts packed in rows, sequence s being rows starts_dev[s] .. starts_dev[s + 1] - 1 (int32,
  *   n_seqs + 1 of them, not decreasing, within [0, T]; lengths of zero are allowed):
@@ -410,7 +410,8 @@ int w4a8_linear_silu_mul_fp8_out(const uint8_t* x8_dev, int64_t M, int64_t K, in
  *   Rows of no sequence (before the first, behind the last) are left as they were.  What a row may not see has no effect on it,
  *   infinities and NaN included.  q_dev [T, H * D], k_dev and v_dev [T, HK * D].  Scores, their maximum and sum and the output's sum are
  *   float32; the weights enter the second product as bf16.  y_scale_dev NULL: y_dev is bf16 [T, H * D].  Otherwise E4M3 bytes, those of
- *   w4a8_quantize_act of that output with *y_scale_dev.  0 < softmax_scale <= 1e30.  T <= 2^24.
+ *   w4a8_quantize_act of that output with *y_scale_dev.  0 < softmax_scale <= 1e30.  T <= 2^24, n_seqs <= 2^20,
+ *   (T / 32 + n_seqs) * H < 2^24.
  *
  * w4a8_attention_decode: one token of each of n_seqs sequences, q_dev [n_seqs, H * D], against the prefix_length tokens that the pages
  *   prefix_pages_dev hold, common to all (computed once for the batch; prefix_length 0: none), followed by the first lengths_dev[b]
@@ -418,11 +419,13 @@ int w4a8_linear_silu_mul_fp8_out(const uint8_t* x8_dev, int64_t M, int64_t K, in
  *   table_width * P.  A page number outside [0, n_pages) holds no tokens.  A sequence without any token gives zeros.  The tokens behind a length may
  *   hold anything.  Precision and y as above.  Lengths, tables and page numbers are read on the device: a captured launch follows them.
  *   workspace_dev: w4a8_attention_decode_workspace_bytes() bytes for these sizes (W4A8_ERR_WORKSPACE if fewer), 16-byte aligned, NULL if that
- *   is 0; scratch, owned by the call until the stream work completes; calls that may overlap need one each.  n_seqs * H <= 2^18.
+ *   is 0; scratch, owned by the call until the stream work completes; calls that may overlap need one each.  n_seqs * H <= 2^18, n_seqs <= 2^20,
+ *   table_width * P and prefix_length <= 2^30.
  *
  * w4a8_cache_copy_pages: page src_pages_dev[i] -> dst_pages_dev[i], page_bytes bytes (a multiple of 16), in each of n_planes planes (keys
  *   and values of every layer, say): page p of plane l at l * plane_stride + p * page_stride bytes.  The destinations of a call are
- *   distinct and none of them is also a source.  A pair with a page outside [0, n_pages) is skipped.  n_copies <= n_pages.
+ *   distinct and none of them is also a source.  A pair with a page outside [0, n_pages) is skipped.  n_copies <= n_pages <= 2^30,
+ *   page_bytes <= 2^30, n_copies times the 32-KiB pieces of a page < 2^24, n_planes <= 65535, strides <= 2^46 bytes.
  */
 typedef enum { W4A8_CACHE_BF16 = 0, W4A8_CACHE_E4M3 = 1, W4A8_CACHE_RANGE_LO = -0x7FFFFFFF - 1, W4A8_CACHE_RANGE_HI = 0x7FFFFFFF } w4a8_cache_dtype;
 typedef enum { W4A8_ROPE_HALVES = 0, W4A8_ROPE_PAIRS = 1, W4A8_ROPE_RANGE_LO = -0x7FFFFFFF - 1, W4A8_ROPE_RANGE_HI = 0x7FFFFFFF } w4a8_rope;

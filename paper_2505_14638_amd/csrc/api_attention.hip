@@ -58,7 +58,8 @@ size_t decode_partial_bytes(const DecodePlan& p, int64_t n_seqs, int q_heads, in
 namespace {
 
 constexpr int64_t TOKENS_MAX = (int64_t)1 << 24, LD_MAX = (int64_t)1 << 20, PAGES_MAX = (int64_t)1 << 30, SEQS_MAX = (int64_t)1 << 20;
-constexpr int64_t WORKGROUPS_MAX = (int64_t)1 << 24;             // of 256 threads: a launch stays below 2^32 threads
+constexpr int64_t WORKGROUPS_MAX = ((int64_t)1 << 24) - 1;       // of 256 threads: a launch stays below 2^32 threads
+constexpr int64_t DECODE_ROWS_MAX = (int64_t)1 << 18;            // up to 64 ranges of each, and as many workgroups again to join them
 
 inline bool aligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
 
@@ -178,7 +179,7 @@ static int check_decode(int64_t n_seqs, int32_t q_heads, int32_t kv_heads, int32
                         int64_t prefix_length) {
     if (int e = check_heads(q_heads, kv_heads, head_dim)) return e;
     if (page_size < 16 || page_size > 1024 || (page_size & (page_size - 1))) return W4A8_ERR_SHAPE;
-    if (n_seqs < 0 || n_seqs > SEQS_MAX || n_seqs * q_heads > WORKGROUPS_MAX / 64 || table_width < 0 || table_width > PAGES_MAX / page_size ||
+    if (n_seqs < 0 || n_seqs > SEQS_MAX || n_seqs * q_heads > DECODE_ROWS_MAX || table_width < 0 || table_width > PAGES_MAX / page_size ||
         prefix_length < 0 || prefix_length > PAGES_MAX)
         return W4A8_ERR_SHAPE;
     return W4A8_OK;
