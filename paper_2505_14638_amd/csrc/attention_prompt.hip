@@ -85,26 +85,32 @@ __device__ __forceinline__ bool find_tile(const int32_t* starts, int n_seqs, int
     return false;
 }
 
-// What becomes of two bf16 values in a walk: themselves; zero instead of what is no number; or one for +infinity (-infinity) and NaN and zero
-// for all else.
-enum Walk { PLAIN = 0, NUMBERS = 1, PLUS = 2, MINUS = 3 };
-__device__ __forceinline__ uint32_t seen_by(int walk, uint32_t w) {
-    uint32_t r = 0;
-#pragma unroll
-    for (int u = 0; u < 32; u += 16) {
-        const uint32_t x = (w >> u) & 0xFFFFu;
-        const bool none = (x & 0x7F80u) == 0x7F80u, nan = none && (x & 0x7Fu);
-        if (walk == NUMBERS) r |= (none ? 0u : x) << u;
-        else r |= (nan || (none && (int)(x >> 15) == walk - PLUS) ? 0x3F80u : 0u) << u;
+// What becomes of two bf16 values in a walk: themselves; zero instead of what is no number; or one for +infinity (-infinity, either) and NaN and
+// zero for all else.
+enum Walk { PLAIN = 0, NUMBERS = 1, PLUS = 2, MINUS = 3, ANY = 4 };
+struct SeenBy {
+    uint32_t first, second, kept, marked;                        // wave-uniform
+    __device__ __forceinline__ explicit SeenBy(int walk) {
+        asm volatile("" : "+s"(walk));                           // (none of it is kept in registers through walks that do without)
+        first = walk == MINUS ? 0xFF80u : 0x7F80u;
+        second = walk == PLUS ? 0x7F80u : 0xFF80u;
+        kept = walk == NUMBERS ? 0xFFFFu : 0;
+        marked = walk == NUMBERS ? 0 : 0x3F80u;
     }
-    return r;
-}
+    __device__ __forceinline__ uint32_t one(uint32_t x) const {
+        const bool hit = (x & 0x7FFFu) > 0x7F80u | x == first | x == second;
+        return hit ? marked : x & kept;
+    }
+    __device__ __forceinline__ uint32_t two(uint32_t w) const { return one(w & 0xFFFFu) | one(w >> 16) << 16; }
+};
 
 // SHARE wavefronts share 32 rows and take a part of every tile's keys each.  A tile of 64 keys takes four wavefronts of 32 rows of 128 channels 32
 // matrix instructions each and about 130 vector instructions, 1.85 us for the two workgroups of a compute unit together.  Copies are asked
-// for a whole tile ahead and waited for at its start; masks are touched only in tiles that hide something.
+// for a whole tile ahead and waited for at its start; masks are touched only in tiles that hide something.  The compiler is told how many wavefronts a
+// vector unit gets at most: with 64 channels it hopes for a fourth, and then saves registers by waiting for each operand by itself (2000 tokens,
+// 8 heads: 20.6 us, so 21.4).
 template <int D, int SHARE, bool CAUSAL, typename OutT>
-__global__ void __launch_bounds__(256, 2) attention_prompt_kernel(PromptArgs a, int tiles, int by_head) {
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, D == 64 ? 3 : 2))) attention_prompt_kernel(PromptArgs a, int tiles, int by_head) {
     constexpr int WAVES = 4, BN = TILE_KEYS, KEYS = BN / SHARE;
     using Block = RowBlock<D, KEYS>;
     constexpr int BM = 32 * WAVES / SHARE, ROW = Block::ROW, PIECES = Block::PIECES, TILE = Block::TILE, RPC = Block::RPC;
@@ -173,8 +179,9 @@ __global__ void __launch_bounds__(256, 2) attention_prompt_kernel(PromptArgs a, 
                 lds_dma_16(vt_base, v_at, here + TILE);
             } else {
                 u32x4 v = *reinterpret_cast<const u32x4*>(vt_base + v_at);
+                const SeenBy seen(walk);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = seen_by(walk, v[i]);
+                for (int i = 0; i < 4; ++i) v[i] = seen.two(v[i]);
                 lds_write(here + TILE + lane * 16, v);
             }
         }
@@ -194,8 +201,10 @@ __global__ void __launch_bounds__(256, 2) attention_prompt_kernel(PromptArgs a, 
     }
 
     // A weight of zero takes a key out of the sums, unless its value is no number.  So if an output is none, the rows are walked again with zeros
-    // for such values, and then twice to mark the outputs that see one: all scores are zero there, and every row counts the ones it sees.  Scores that
-    // are NaN or +infinity are NaN there: such a row's outputs are NaN already, its counts too, and no value changes that.
+    // for such values, and then to mark the outputs that see one: all weights are one there, and every row counts the ones it sees.  PLUS and MINUS leave
+    // out scores of -infinity, whose weights are zero by definition and not for want of bits; such a weight makes NaN of an infinity, so ANY
+    // counts under these scores alone.  Scores that are NaN or +infinity are NaN there: such a row's outputs are NaN already, its counts too, and
+    // no value changes that.
     uint64_t marked = 0;                                         // outputs of this lane that see +infinity or NaN
     for (;; ++walk) {
     rows.clear();
@@ -209,26 +218,26 @@ __global__ void __launch_bounds__(256, 2) attention_prompt_kernel(PromptArgs a, 
         if (CAUSAL && key0 > q0 + 32 * band + 31) return;        // (wave-uniform) no row of this wavefront sees its keys of the tile
         v16f s[KT];
         rows.template scores<buffer>(s);
-        for (int counts = uniform(walk >= PLUS); counts;) {      // (a loop of at most one pass, as below)
-#pragma unroll
-            for (int k = 0; k < KT; ++k)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[k][r] = s[k][r] == NEG_INF ? 0.0f : s[k][r] * 0.0f;
-            asm volatile("s_mov_b32 %0, 0" : "=s"(counts));
-        }
         const bool masked = key0 + KEYS > len || (CAUSAL && key0 + KEYS - 1 > q0 + 32 * band);
         const int seen = CAUSAL ? min(len, row + 1) : len;       // keys below this one
         // a loop of at most one pass: as a branch the compiler turns it into 32 comparisons and selects in every tile
-        int hides = uniform(masked);
-        while (hides) {
-            int edge = seen - key0 - 4 * half;
-            asm volatile("" : "+v"(edge));
+        int changes = uniform(masked || walk >= PLUS);
+        while (changes) {
+            int edge = seen - key0 - 4 * half, now = walk;
+            asm volatile("" : "+v"(edge), "+s"(now));
+            if (now >= PLUS) {
+                const float at_inf = now == ANY ? 0.0f : NEG_INF, else_at = now == ANY ? NEG_INF : 0.0f;
+#pragma unroll
+                for (int k = 0; k < KT; ++k)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[k][r] = s[k][r] == NEG_INF ? at_inf : fmaf(s[k][r], 0.0f, else_at);
+            }
 #pragma unroll
             for (int k = 0; k < KT; ++k)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if (32 * k + (r & 3) + 8 * (r >> 2) >= edge) s[k][r] = NEG_INF;
-            asm volatile("s_mov_b32 %0, 0" : "=s"(hides));
+            asm volatile("s_mov_b32 %0, 0" : "=s"(changes));
         }
         uint32_t p[KT][8];
         rows.weights(s, a.scale_log2, p);
@@ -309,18 +318,13 @@ __global__ void __launch_bounds__(256, 2) attention_prompt_kernel(PromptArgs a, 
             const int r = i / EACH * (64 / LANES) + lane / LANES, c = piece * EACH + i % EACH;
             const uint16_t count = lds_read<uint16_t>(slab + r * ROW + (uint32_t)(((c / 8) ^ swizzle<D>(r)) << 4) + c % 8 * 2);
             if (count == 0 || (count & 0x7FFFu) > 0x7F80u || q0 + 32 * band + r >= len) continue;
-            OutT* at = y + (int64_t)r * a.ldy + i % EACH;
-            if (walk == PLUS) {
-                marked |= (uint64_t)1 << i;
-                *at = BYTES ? (OutT)quantize_one(-NEG_INF, quant.s) : (OutT)0x7F80;
-            } else {
-                const bool both = marked >> i & 1;
-                *at = BYTES ? (OutT)quantize_one(both ? __builtin_nanf("") : NEG_INF, quant.s) : (OutT)(both ? 0x7FC0 : 0xFF80);
-            }
+            const float becomes = walk == PLUS ? -NEG_INF : walk == ANY || (marked >> i & 1) ? __builtin_nanf("") : NEG_INF;
+            if (walk == PLUS) marked |= (uint64_t)1 << i;
+            y[(int64_t)r * a.ldy + i % EACH] = BYTES ? (OutT)quantize_one(becomes, quant.s) : (OutT)(__float_as_uint(becomes) >> 16);
         }
     }
     }
-    if (walk == PLAIN || walk == MINUS) break;
+    if (walk == PLAIN || walk == ANY) break;
     __syncthreads();                                             // all have read what the next walk's tiles replace
     }
 }

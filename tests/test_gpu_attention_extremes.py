@@ -113,3 +113,22 @@ def test_weights_of_a_row_come_to_one(gpu_lib, d, spread):
                 scales[1] = 2.0
             y = B.attention_decode(q[:len(lengths)], k, v, ints(tables), ints(lengths), ints(prefix_pages) if prefix else None, prefix, scales)
             assert (y == 1).all(), (cache, lengths, prefix)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("t,hq,hk,d", SIZES)
+def test_infinite_values_under_infinite_scores(gpu_lib, t, hq, hk, d, causal):
+    """A weight of exactly zero, that of a score of -infinity, makes NaN of an infinite value; a weight that is only small does not."""
+    q, k, v = prompt_inputs(47, t, hq, hk, d)
+    q[..., 0] = q[..., 0].abs() + 0.1
+    k[..., 0] = 0.25
+    v = infinite_values(v, 30)
+    for at in (30, 35, 33):                                      # under both, one of a pair, neither
+        bad = k.clone()
+        bad[at, 0, 0] = -INF
+        check_prompt(q, bad, v, causal, heads_of(hq))
+    far = k.clone()
+    far[30, 0, 0] = -1500.0                                      # a weight of about e^-200 or less: zero in 32 bits, not in 64
+    far_q = q.clone()
+    far_q[..., 0] = 2.0 if d == 128 else 1.25
+    check_prompt(far_q, far, v, causal, heads_of(hq))
