@@ -408,7 +408,8 @@ int w4a8_linear_silu_mul_fp8_out(const uint8_t* x8_dev, int64_t M, int64_t K, in
  *   n_seqs + 1 of them, not decreasing, within [0, T]; lengths of zero are allowed):
  *     y[i] = sum_j softmax_j(softmax_scale * q[i] . k[j]) v[j]  over the rows j of i's sequence, j <= i if causal = 1.
  *   Rows of no sequence (before the first, behind the last) are left as they were.  What a row may not see has no effect on it,
- *   infinities and NaN included.  q_dev [T, H * D], k_dev and v_dev [T, HK * D].  Scores, their maximum and sum and the output's sum are
+ *   infinities and NaN included; among what it sees they do what the formula says: a score of -infinity has a weight of zero, a row of such scores
+ *   alone is NaN.  q_dev [T, H * D], k_dev and v_dev [T, HK * D].  Scores, their maximum and sum and the output's sum are
  *   float32; the weights enter the second product as bf16.  y_scale_dev NULL: y_dev is bf16 [T, H * D].  Otherwise E4M3 bytes, those of
  *   w4a8_quantize_act of that output with *y_scale_dev.  0 < softmax_scale <= 1e30.  T <= 2^24, n_seqs <= 2^20,
  *   (T / 32 + n_seqs) * H < 2^24.
@@ -416,7 +417,8 @@ int w4a8_linear_silu_mul_fp8_out(const uint8_t* x8_dev, int64_t M, int64_t K, in
  * w4a8_attention_decode: one token of each of n_seqs sequences, q_dev [n_seqs, H * D], against the prefix_length tokens that the pages
  *   prefix_pages_dev hold, common to all (computed once for the batch; prefix_length 0: none), followed by the first lengths_dev[b]
  *   tokens (int32) of the pages of its own table, row b of tables_dev [n_seqs, table_width], row stride ld_tables.  Lengths count up to
- *   table_width * P.  A page number outside [0, n_pages) holds no tokens.  A sequence without any token gives zeros.  The tokens behind a length may
+ *   table_width * P.  A page number outside [0, n_pages) holds no tokens.  A sequence without any token gives zeros (one whose
+ *   tokens all have scores of -infinity is NaN).  The tokens behind a length may
  *   hold anything.  Precision and y as above.  Lengths, tables and page numbers are read on the device: a captured launch follows them.
  *   workspace_dev: w4a8_attention_decode_workspace_bytes() bytes for these sizes (W4A8_ERR_WORKSPACE if fewer), 16-byte aligned, NULL if that
  *   is 0; scratch, owned by the call until the stream work completes; calls that may overlap need one each.  n_seqs * H <= 2^18, n_seqs <= 2^20,

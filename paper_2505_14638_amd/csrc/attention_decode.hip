@@ -211,6 +211,13 @@ __device__ __forceinline__ void stream_keys(const DecodeArgs& a, const DecodePla
         key += STRIDE;
     }
 
+    if (__builtin_amdgcn_ballot_w64(m == NEG_INF)) {             // no tokens, or no score above -infinity?
+        bool saw = false;
+        for (key = k_begin + STEP * wave; key < k_end && !saw; key += STRIDE)
+            for (int64_t at = key; at < key + STEP && at < k_end; at += 16) saw |= (uint32_t)pages[at >> a.c.page_shift] < a.c.n_pages;
+        if (saw) m = fmaxf(m, LOWEST);
+    }
+
     // the wavefronts' results joined
     l = sum_over_32(sum_over_16(l));
 #pragma unroll
@@ -246,7 +253,7 @@ __device__ __forceinline__ void stream_keys(const DecodeArgs& a, const DecodePla
     const int r = first_row + out_row;
     const int64_t at = (int64_t)(r / group) * a.q_heads + kv_head * group + r % group;   // (sequence, query head)
     if constexpr (!std::is_void_v<OutT>) {
-        const float inv = inverse_sum(sum);
+        const float inv = inverse_sum(top, sum);
         const Bf16Quantizer quant(a.y_scale ? *a.y_scale : 1.0f);
         OutT* y = static_cast<OutT*>(a.y) + (int64_t)(r / group) * a.ldy + (int64_t)(kv_head * group + r % group) * D + ch;
 #pragma unroll
@@ -420,6 +427,11 @@ __device__ __forceinline__ void walk_prefix(const DecodeArgs& a, const DecodePla
         if (t + 1 < t_end) step(t + 1, std::integral_constant<int, 1>{});
     }
     const float sum = sum_over_32(rows.l), v_scale = E4M3 ? a.kv_scales[1] : 1.0f;
+    if (__builtin_amdgcn_ballot_w64(rows.m == NEG_INF)) {        // no tokens, or no score above -infinity?
+        bool saw = false;
+        for (int t = t_begin; t < t_end && !saw; ++t) saw = __builtin_amdgcn_ballot_w64(pages_of(t) >= 0);
+        if (saw) rows.m = fmaxf(rows.m, LOWEST);
+    }
     const int r = first + col;
     if (r >= n_rows) return;
     const int64_t total = (int64_t)a.n_seqs * a.q_heads, part = plan.own_splits + split;
@@ -508,7 +520,7 @@ __global__ void __launch_bounds__(256) attention_join_kernel(DecodeArgs a, int p
             }
         }
     }
-    const float inv = inverse_sum(sum);
+    const float inv = inverse_sum(top, sum);
 #pragma unroll
     for (int j = 0; j < VD; ++j) acc[j] = sum_over_32(sum_over_16(acc[j])) * inv;
     if constexpr (WAVES > 1) {

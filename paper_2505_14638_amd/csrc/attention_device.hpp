@@ -61,8 +61,10 @@ __device__ __forceinline__ float add_pair(uint32_t w, float c) {
 // large, so that the sums are seldom scaled again.  Weights up to 2^RISE lose nothing in float32 or bf16.
 constexpr float RISE = 8.0f;
 
-// 1 / sum of a finished row; a row that saw nothing (sum 0) gives zeros.
-__device__ __forceinline__ float inverse_sum(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+// 1 / sum of a finished row of decoding.  Maxima are -infinity only where there are no tokens, LOWEST if tokens have scores of -infinity alone: the
+// first gives zeros, the second NaN like 0 / 0.  In a join either counts nothing beside other scores.
+constexpr float LOWEST = -3.402823466e38f;
+__device__ __forceinline__ float inverse_sum(float m, float l) { return m == NEG_INF ? 0.0f : 1.0f / l; }
 
 // h / s rounded to float32 and then to E4M3, as the activation quantization does it, for values h that are bf16: two instructions a quotient.
 // high + low is 1 / s up to 2^-45 of it, so h * low + h * high rounds as h / s does, unless h / s lies within 2^-45 of the middle of two

@@ -283,7 +283,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, D =
                 }
         }
     }
-    const float inv = inverse_sum(total);
+    // (every row sees itself: a sum of zero is one of scores of -infinity alone, NaN like 0 / 0.  In a mark's walk a row may count nothing)
+    const float inv = walk >= PLUS ? 1.0f : 1.0f / total;
     const uint32_t slab = lds_base + band * 32 * ROW;
     if (part == 0) {
 #pragma unroll

@@ -132,3 +132,58 @@ def test_infinite_values_under_infinite_scores(gpu_lib, t, hq, hk, d, causal):
     far_q = q.clone()
     far_q[..., 0] = 2.0 if d == 128 else 1.25
     check_prompt(far_q, far, v, causal, heads_of(hq))
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("t,hq,hk,d", SIZES)
+def test_infinite_scores(gpu_lib, t, hq, hk, d, causal):
+    """Keys with an infinity: scores of +infinity make a row NaN; those of -infinity count nothing, unless a row has no others (NaN, as 0 / 0 is)."""
+    q, k, v = prompt_inputs(43, t, hq, hk, d)
+    q[::3, :, 0], k[0:40, 0, 0], k[40:, 1, 0] = q[::3, :, 0].abs(), -INF, INF
+    check_prompt(q, k, v, causal, heads_of(hq))
+    k[:, :, 0] = -INF
+    check_prompt(q, k, infinite_values(v, 30), causal, heads_of(hq))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lengths,prefix,hq,hk", [
+    ([40, 0, 5], 0, 4, 2), ([700, 0, 33], 0, 4, 2), ([20] * 300, 0, 4, 4), ([600, 0, 3], 50, 4, 2), ([5, 0] * 15, 330, 8, 2), ([0] * 30, 330, 8, 2),
+])
+def test_decode_of_rows_without_a_weight(gpu_lib, lengths, prefix, hq, hk, d, cache):
+    """Rows with tokens whose scores are all -infinity give NaN, those without any token zeros; in each kernel, with one part and with several."""
+    n = len(lengths)
+    k, v, scales, tables, prefix_pages = paged(17, lengths, prefix, hk, d, 16, cache)
+    one = 1.0 if cache == "bf16" else 0x38
+    k[..., 0] = one
+    q = randn(5, n, hq, d).bfloat16()
+    args = dict(prefix_pages=ints(prefix_pages) if prefix else None, prefix_length=prefix, kv_scales=scales)
+    usual = B.attention_decode(q, k, v, ints(tables), ints(lengths), **args)
+    told = q.clone()
+    told[:, 1, 3] = 0.0                                          # (its neighbour is changed too, and stays finite)
+    told[:, 0, 0] = -INF
+    y = B.attention_decode(told, k, v, ints(tables), ints(lengths), **args).view(n, hq, d)
+    seen = torch.tensor([x + prefix > 0 for x in lengths])
+    assert torch.isnan(y[seen, 0]).all() and (y[~seen] == 0).all() and torch.isfinite(y[:, 1:]).all()
+    assert torch.equal(y[:, max(2, hq // hk):], usual.view(n, hq, d)[:, max(2, hq // hk):])
+    # tokens on pages that are none: as if there were no tokens
+    none = [[-1] * len(x) for x in tables]
+    args["prefix_pages"] = ints([-1] * len(prefix_pages)) if prefix else None
+    assert (B.attention_decode(told, k, v, ints(none), ints(lengths), **args) == 0).all()
+
+
+@pytest.mark.parametrize("prefix,n", [(0, 1), (50, 1), (150, 20)])
+def test_decode_of_some_infinite_scores(gpu_lib, prefix, n):
+    """A whole part, and a whole wavefront's keys, of scores of -infinity count nothing beside others."""
+    hq, hk, d = 4, 2, 64
+    lengths = [700] * n
+    k, v, _, tables, prefix_pages = paged(19, lengths, prefix, hk, d, 16, "bf16")
+    q = randn(5, n, hq, d).bfloat16()
+    q[..., 0] = q[..., 0].abs() + 0.1
+    k[[p for x in tables for p in x[:40]], :, :, 0] = -INF       # the first 640 own tokens
+    k[[p for x in tables for p in x[40:]] + prefix_pages, :, :, 0] = 0.25
+    y = B.attention_decode(q, k, v, ints(tables), ints(lengths), ints(prefix_pages) if prefix else None, prefix)
+    places = [prefix_pages[j // 16] * 16 + j % 16 for j in range(prefix)] + [p * 16 + j for p in tables[0] for j in range(16)][:700]
+    kk, vv = (R.cache_values(x).transpose(1, 2).reshape(-1, hk, d)[places] for x in (k, v))
+    for h in range(hq):
+        agrees(y.view(n, hq, d)[:1, h], *defined(R.heads(q[:1].reshape(1, -1), d)[:, h], kk[:, h // 2], vv[:, h // 2], d ** -0.5))
