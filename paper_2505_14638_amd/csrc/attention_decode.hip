@@ -342,19 +342,26 @@ __device__ __forceinline__ void walk_prefix(const DecodeArgs& a, const DecodePla
             }
             const int64_t at = (page * a.c.page_stride + ((int64_t)kv_head * a.c.page_size + (key & (a.c.page_size - 1))) * D) * SIZE;
             const int last = (int)(a.prefix_len - 1 - key);      // of the group's rows, if below 15
+            auto copy = [&](int i, bool ends) {                  // ends: the prefix, in this group
+                const int r = i * RPC + lane / PIECES;
+                const uint32_t off = (uint32_t)((ends ? min(r, last) : r) * ROW + ((lane % PIECES) ^ swizzle<D>(r)) * 16);
+                lds_dma_16(a.k_cache + at, off, to + i * 1024);
+                if (!ends) lds_dma_16(a.v_cache + at, off, to + TILE + i * 1024);
+                else lds_write(to + TILE + i * 1024 + lane * 16, r > last ? u32x4{0, 0, 0, 0} : *reinterpret_cast<const u32x4*>(a.v_cache + at + off));
+            };
+            if (E4M3) {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                if (E4M3) {
+                for (int i = 0; i < LOADS; ++i) {
                     const int byte = (i * 64 + lane) * 16, r = min(byte / D, last);
                     held[2 * LOADS * g + i] = *reinterpret_cast<const u32x4*>(a.k_cache + at + r * D + byte % D);
                     held[2 * LOADS * g + LOADS + i] = *reinterpret_cast<const u32x4*>(a.v_cache + at + r * D + byte % D);
-                } else {
-                    const int r = i * RPC + lane / PIECES;
-                    const uint32_t off = (uint32_t)(min(r, last) * ROW + ((lane % PIECES) ^ swizzle<D>(r)) * 16);
-                    lds_dma_16(a.k_cache + at, off, to + i * 1024);
-                    if (last >= 15) lds_dma_16(a.v_cache + at, off, to + TILE + i * 1024);
-                    else lds_write(to + TILE + i * 1024 + lane * 16, r > last ? u32x4{0, 0, 0, 0} : *reinterpret_cast<const u32x4*>(a.v_cache + at + off));
                 }
+            } else if (last >= 15) {
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) copy(i, false);
+            } else {
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) copy(i, true);
             }
         }
     };
