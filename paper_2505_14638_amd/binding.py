@@ -689,7 +689,7 @@ def attention_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
                      workspace: torch.Tensor | None = None) -> torch.Tensor:
     """w4a8_attention_decode: q bf16 [sequences, H, D], caches [pages, HK, page_size, D], tables int32 [sequences, width], lengths int32
     [sequences], prefix_pages int32 with ceil(prefix_length / page_size) entries.  Returns bf16 [sequences, H * D], or with y_scale
-    E4M3 bytes (uint8).  workspace: uint8, attention_decode_workspace_bytes() of them; allocated here if None."""
+    E4M3 bytes (uint8).  workspace: contiguous uint8, attention_decode_workspace_bytes() of them; allocated here if None."""
     n, hq, d, ldq = _rows(q, "q")
     cache_dtype, n_pages, page_stride, page, hk, dk = _cache_args(k_cache, v_cache, kv_scales)
     rows, width = tables.shape
@@ -707,6 +707,8 @@ def attention_decode(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
         need = lib().w4a8_attention_decode_workspace_bytes(n, hq, hk, d, page, width, prefix_length)
         if need:
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    elif not workspace.is_contiguous():                          # its bytes beside the view are not the call's
+        raise ValueError(f"workspace: contiguous, got {tuple(workspace.shape)} {workspace.stride()}")
     stream = _stream_of(q, k_cache, v_cache, tables, lengths, prefix_pages, kv_scales, out, y_scale, workspace)
     ldy = _flat_rows(out, n, hq * d, dtype, "out")
     _check(lib().w4a8_attention_decode(q.data_ptr(), ldq, n, hq, hk, d, k_cache.data_ptr(), v_cache.data_ptr(), cache_dtype, _pointer(kv_scales),

@@ -1,8 +1,9 @@
-"""Calls at the limits of a launch: 2^32 threads do not fit one, and are refused before anything is enqueued.  No GPU."""
+"""Calls at the limits of a launch and of a workspace: 2^32 threads do not fit one, and are refused before anything is enqueued.  No GPU."""
 import os
 import subprocess
 
 import pytest
+import torch
 
 from paper_2505_14638_amd import binding as B
 
@@ -39,3 +40,12 @@ def test_every_accepted_launch_fits(tmp_path):
     assert build.returncode == 0, build.stdout[-4000:]
     run = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=120)
     assert run.returncode == 0 and "all checks passed" in run.stdout, run.stdout[-4000:]
+
+
+def test_a_workspace_with_holes_is_refused(L):
+    """Every second byte of a buffer, and one byte seen many times, have fewer bytes behind their address than elements."""
+    q, cache = torch.zeros((2, 4, 64), dtype=torch.bfloat16), torch.zeros((5, 2, 16, 64), dtype=torch.bfloat16)
+    tables, lengths = torch.zeros((2, 1), dtype=torch.int32), torch.ones(2, dtype=torch.int32)
+    for work in (torch.zeros(1 << 16, dtype=torch.uint8)[::2], torch.zeros(1, dtype=torch.uint8).expand(1 << 16)):
+        with pytest.raises(ValueError, match="workspace"):
+            B.attention_decode(q, cache, cache, tables, lengths, workspace=work)
