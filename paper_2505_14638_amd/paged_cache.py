@@ -85,26 +85,33 @@ class PagedCache:
                     uses[last] -= 1
                     own[s] = last
             wanted += -(-(n + c) // self.page_size) - len(pages)
-        if wanted + len(own) > len(self._free):
-            raise OutOfPages(f"{wanted + len(own)} pages wanted, {len(self._free)} free")
-        if own:
-            taken = self._free[:-len(own) - 1:-1]
-            B.cache_copy_pages(self.data, self._ints(list(own.values())), self._ints(taken))
-            del self._free[-len(own):]
-            for (s, old), new in zip(own.items(), taken):
-                self._uses[new] = 1
-                self._pages[s][-1] = new
-                self._release(old)
-        positions, slots = [], []
+        wanted += len(own)
+        if wanted > len(self._free):
+            raise OutOfPages(f"{wanted} pages wanted, {len(self._free)} free")
+        fresh = self._free[:-wanted - 1:-1]
+        copies, rest = dict(zip(own, fresh)), iter(fresh[len(own):])
+        positions, slots, ends = [], [], []                      # ends: the pages of each sequence from the first that is not full on
         for s, c in zip(seqs, counts):
-            n, pages = self._length[s], self._pages[s]
-            while len(pages) * self.page_size < n + c:
-                pages.append(self._free.pop())
-                self._uses[pages[-1]] = 1
+            n, full = self._length[s], self._length[s] // self.page_size
+            end = [copies.get(s, p) for p in self._pages[s][full:]]
+            while (full + len(end)) * self.page_size < n + c:
+                end.append(next(rest))
             positions += range(n, n + c)
-            slots += [pages[j // self.page_size] * self.page_size + j % self.page_size for j in range(n, n + c)]
-            self._length[s] = n + c
-        return self._ints(positions), self._ints(slots)
+            slots += [end[j // self.page_size - full] * self.page_size + j % self.page_size for j in range(n, n + c)]
+            ends.append(end)
+        told = self._ints(positions), self._ints(slots)
+        if own:
+            B.cache_copy_pages(self.data, self._ints(list(own.values())), self._ints(fresh[:len(own)]))
+        # the books, after all that can raise
+        del self._free[len(self._free) - wanted:]
+        for p in fresh:
+            self._uses[p] = 1
+        for old in own.values():
+            self._release(old)
+        for s, c, end in zip(seqs, counts, ends):
+            self._pages[s][self._length[s] // self.page_size:] = end
+            self._length[s] += c
+        return told
 
     def tables(self, seqs: list[int], share: bool = True):
         """What w4a8_attention_decode takes for a batch: (tables, lengths, prefix_pages or None, prefix_length).  share: the full pages that
