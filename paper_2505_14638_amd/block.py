@@ -166,7 +166,11 @@ class DecoderBlock(DecoderBlockLinears):
     def forward_prompt(self, x: torch.Tensor, starts: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor, cache,
                        keep: dict | None = None) -> torch.Tensor:
         """Whole prompts, packed: x bf16 [M, hidden], starts int32 [sequences + 1] (rows of no sequence get what their buffer held);
-        positions and slots int32 [M], where each token goes in `cache` = (keys, values, scales or None)."""
+        positions and slots int32 [M], where each token goes in `cache` = (keys, values, scales or None).  A row attends to rows of this call
+        alone, so its sequence holds nothing before them: PagedCache.grow's positions behind tokens are refused (a copy of them is not known as such).
+        Sequences that hold tokens take further ones by forward_decode, or by a prompt of all of them as a new sequence."""
+        if getattr(positions, "behind_tokens", False):
+            raise ValueError("forward_prompt: a sequence holds tokens already, which its new rows would not see")
         m, (k_cache, v_cache, kv_scales) = x.shape[0], cache
         qkv = self._qkv(x, m, keep)
         q, k = self._rows("q", m, self.heads), self._rows("k", m, self.kv_heads)

@@ -72,7 +72,7 @@ class PagedCache:
 
     def grow(self, seqs: list[int], counts: list[int]):
         """Room for counts[i] further tokens of seqs[i] (distinct): (positions, slots), int32 on the device, of all of them in order, as
-        w4a8_rope_cache_write takes them."""
+        w4a8_rope_cache_write takes them.  positions.behind_tokens says whether any of them come behind tokens that the sequence holds already."""
         if len(set(seqs)) != len(seqs) or len(seqs) != len(counts) or any(c < 0 for c in counts):
             raise ValueError("distinct sequences with a count >= 0 each")
         own, wanted = {}, 0                                      # sequences whose last page has to become their own
@@ -100,6 +100,7 @@ class PagedCache:
             slots += [end[j // self.page_size - full] * self.page_size + j % self.page_size for j in range(n, n + c)]
             ends.append(end)
         told = self._ints(positions), self._ints(slots)
+        told[0].behind_tokens = any(c and self._length[s] for s, c in zip(seqs, counts))
         if own:
             B.cache_copy_pages(self.data, self._ints(list(own.values())), self._ints(fresh[:len(own)]))
         # the books, after all that can raise
