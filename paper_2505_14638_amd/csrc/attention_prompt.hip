@@ -110,7 +110,7 @@ struct SeenBy {
 // vector unit gets at most: with 64 channels it hopes for a fourth, and then saves registers by waiting for each operand by itself (2000 tokens,
 // 8 heads: 20.6 us, so 21.4).
 template <int D, int SHARE, bool CAUSAL, typename OutT>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, D == 64 ? 3 : 2))) attention_prompt_kernel(PromptArgs a, int tiles, int by_head) {
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, D == 64 ? 3 : 2))) attention_prompt_kernel(PromptArgs a, int by_head) {
     constexpr int WAVES = 4, BN = TILE_KEYS, KEYS = BN / SHARE;
     using Block = RowBlock<D, KEYS>;
     constexpr int BM = 32 * WAVES / SHARE, ROW = Block::ROW, PIECES = Block::PIECES, TILE = Block::TILE, RPC = Block::RPC;
@@ -336,8 +336,8 @@ void launch_tile(const PromptArgs& a, hipStream_t st) {
     const int64_t tiles = a.n_seqs == 1 ? (a.T + BM - 1) / BM : a.T / BM + a.n_seqs;   // at most
     const int by_head = a.kv_heads % XCDS_A == 0;
     const dim3 grid((unsigned)(tiles * a.q_heads)), block(256);
-    if (a.y_scale) hipLaunchKernelGGL((attention_prompt_kernel<D, SHARE, CAUSAL, uint8_t>), grid, block, 0, st, a, (int)tiles, by_head);
-    else hipLaunchKernelGGL((attention_prompt_kernel<D, SHARE, CAUSAL, uint16_t>), grid, block, 0, st, a, (int)tiles, by_head);
+    if (a.y_scale) hipLaunchKernelGGL((attention_prompt_kernel<D, SHARE, CAUSAL, uint8_t>), grid, block, 0, st, a, by_head);
+    else hipLaunchKernelGGL((attention_prompt_kernel<D, SHARE, CAUSAL, uint16_t>), grid, block, 0, st, a, by_head);
 }
 
 // Workgroups of 128 rows read least; but a wavefront's way through a tile is one chain of instructions that wait for each other, and with
