@@ -389,7 +389,7 @@ int w4a8_linear_silu_mul_fp8_out(const uint8_t* x8_dev, int64_t M, int64_t K, in
  *   cache       keys and values each in pages of P tokens, a page [HK, P, D] row-major, page p at p * page_stride elements
  *               (page_stride >= HK * P * D, whole 16-byte pieces; 16-byte aligned); P a power of two, 16 .. 1024; n_pages * P <= 2^30.
  *               Elements bf16, or E4M3 bytes that stand for byte * kv_scales_dev[0] (keys), byte * kv_scales_dev[1] (values): static
- *               per-tensor scales, as for activations (Eq. 13).  kv_scales_dev is read for E4M3 only
+ *               per-tensor scales, as for activations (Eq. 13), finite and above zero.  kv_scales_dev is read for E4M3 only
  *   tables_dev  int32 page numbers: position j of a sequence is token j % P of page table[j / P].  Sequences may list the same page
  *   rows        row strides (ld*) in elements, below 2^20; rows are 16-byte aligned (pointer and stride).  Outputs overlap no input, save where it is
  *               said
@@ -410,7 +410,8 @@ int w4a8_linear_silu_mul_fp8_out(const uint8_t* x8_dev, int64_t M, int64_t K, in
  *   Rows of no sequence (before the first, behind the last) are left as they were.  What a row may not see has no effect on it,
  *   infinities and NaN included; among what it sees they do what the formula says: a score of -infinity has a weight of zero, a row of such scores
  *   alone is NaN.  q_dev [T, H * D], k_dev and v_dev [T, HK * D].  Scores, their maximum and sum and the output's sum are
- *   float32; the weights enter the second product as bf16.  y_scale_dev NULL: y_dev is bf16 [T, H * D].  Otherwise E4M3 bytes, those of
+ *   float32; the weights enter the second product, and their sum, as bf16.  The output's sum is formed under weights of up to 2^8 and divided
+ *   at last: it stays finite for |v| < 2^88.  y_scale_dev NULL: y_dev is bf16 [T, H * D].  Otherwise E4M3 bytes, those of
  *   w4a8_quantize_act of that output with *y_scale_dev.  0 < softmax_scale <= 1e30.  T <= 2^24, n_seqs <= 2^20,
  *   (T / 32 + n_seqs) * H < 2^24.
  *

@@ -13,7 +13,8 @@ copy of the gate|up weights) and, up to eight tokens, the quantization of the bl
 same block output.
 
 `DecoderBlock` has attention in that place: queries and keys are rotated, keys and values go to a paged cache, and whole prompts or single
-tokens of a batch attend; with `fused=True` attention writes the E4M3 bytes that the O projection reads.
+tokens of a batch attend; with `fused=True` attention writes the E4M3 bytes that the O projection reads.  Neither class has norms or residual
+additions: they are the quantized layers, and attention, of a block.
 """
 from __future__ import annotations
 

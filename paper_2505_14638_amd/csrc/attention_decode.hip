@@ -455,7 +455,7 @@ __device__ __forceinline__ void walk_prefix(const DecodeArgs& a, const DecodePla
 
 // The prefix for many rows and the sequences' own tokens in one launch: the workgroups on the prefix come first, mostly one for every
 // compute unit or fewer, and those on the own tokens, which memory bounds, run beside them.  256 sequences, 64 heads, 8191 E4M3 tokens in
-// common and 30 .. 1000 of their own: 121 us, where the two take 105 and 62 apart; with twice the workgroups on the prefix, which then leave
+// common and 30 .. 1000 of their own: 124 us, where the two take 105 and 62 apart; with twice the workgroups on the prefix, which then leave
 // no room beside them, 156.
 template <int D, bool E4M3>
 __global__ void __launch_bounds__(64 * WAVES_D, 2) attention_shared_kernel(DecodeArgs a, DecodePlan plan, int own_units, int row_tiles, int units,

@@ -4,9 +4,9 @@
 // sequence's keys 64 at a time (attention_tile.hpp).  Keys and values come to LDS by copies that pass no registers, one tile ahead.  Two
 // workgroups share a compute unit (64 KB of LDS and 256 registers a lane each), so that one forms weights while the other multiplies.
 // One prompt of 8192 tokens, 32 query and 8 key heads of 128 channels, causal: 500 us, 1100 TFLOP/s of the products that the mask leaves; a
-// bf16 product of 8192 x 8192 x 8192 reaches 1190 here, so the matrix cores bound it.  Thirteen prompts of 1 .. 1531 tokens: 128 us, 700
+// bf16 product of 8192 x 8192 x 8192 reaches 1190 here, so the matrix cores bound it.  Thirteen prompts of 1 .. 1531 tokens: 129 us, 700
 // TFLOP/s; there a workgroup's start (2.4 us to its tile, 1.5 to its rows) and end (2 .. 4) stand against 20 us of products, half hidden behind
-// the other workgroup's.  Both ways, three sequences of 700 .. 1500, 16 heads of 64 channels: 34.6 us, 590 TFLOP/s: fewer workgroups (496)
+// the other workgroup's.  Both ways, three sequences of 700 .. 1500, 16 heads of 64 channels: 34.3 us, 590 TFLOP/s: fewer workgroups (496)
 // than there are places, the longest sequence's set the time, and half as many products for each exponential.
 #include "attention.hpp"
 #include "attention_tile.hpp"
@@ -31,7 +31,8 @@ __device__ __forceinline__ int wave_sum(int x) { return wave_reduce<false>(x); }
 
 // Unit t (0 .. tiles - 1) of the packed batch: a sequence and a tile of its rows; false behind the last.  Causal tiles cost what their place
 // in the sequence says, so up to 64 sequences (a lane each) give their tiles in falling order of it, all the sequences' together: the
-// long ones start first.  More sequences come one after the other, each from its end.
+// long ones start first.  More sequences come one after the other, each from its end, and every workgroup looks through them 64 at a time: 64
+// prompts of 20 .. 60 tokens, 32 heads, 27.3 us, 65 of them 29.7, 300 150, 1000 of 1 .. 60 724.
 template <int BM>
 __device__ __forceinline__ bool find_tile(const int32_t* starts, int n_seqs, int64_t T, int t, int& seq_start, int& len, int& tile) {
     const int lane = threadIdx.x & 63;
@@ -342,8 +343,9 @@ void launch_tile(const PromptArgs& a, hipStream_t st) {
 
 // Workgroups of 128 rows read least; but a wavefront's way through a tile is one chain of instructions that wait for each other, and with
 // hardly more than one workgroup per compute unit nothing else fills those waits.  Then 64 rows a workgroup, two wavefronts on each 32: one
-// prompt of 512 tokens, 32 heads, 14.2 -> 13.2 us (128 workgroups of 128 rows), of 1100 27.1 -> 24.3 (288), of 2000 on 8 heads of 64 channels
-// 28.9 -> 22.7 (128).  Three of 700 .. 1500 on 16 heads of 64 channels (432) lose, 37 -> 44.
+// prompt of 512 tokens, 32 heads, 14.0 -> 12.4 us (128 workgroups of 128 rows), of 1100 26.5 -> 23.1 (288), of 1536 34.2 -> 31.2 (384), of 2000 on 8
+// heads of 64 channels 27.7 -> 20.8 (128).  Of 1700 (448) it would gain still, 38.7 -> 37.3, but three sequences of 700 .. 1500 on 16 heads of 64
+// channels, both ways (432), lose, 34.4 -> 40.5, and 40 of 1 .. 300 (1505) 43.7 -> 56.6.
 constexpr int FEW = 384;
 template <int D, bool CAUSAL>
 void launch_rows(const PromptArgs& a, hipStream_t st) {
